@@ -1,0 +1,133 @@
+// What the attention kernels over a paged cache share: the call's arguments
+// on the device, the rows and the cached tokens of a block, and who sees
+// whom.
+#pragma once
+
+#include "device_common.h"
+#include "paged.h"
+
+namespace starkv {
+
+struct AttendArgs {
+  const char* q;
+  char* out;
+  float* lse;
+  float* part;            // partial outputs, [units][n_split][row_tile][d]
+  float2* stat;           // partial (max, sum), [units][n_split][row_tile]
+  const uint64_t* mask;
+  int words, window, sinks;
+  int n_split, chunk, n_tiles, n_rows;
+  float scale;            // log2(e) / sqrt(d)
+};
+
+struct AttendLists {      // with PagedView and AttendArgs below 4 KB of kernel arguments
+  RowList r;
+  int32_t tile0[kMaxSeqs + 1];
+};
+
+// The last b with first[b] <= k: the sequence of row tile k (sequences
+// without rows have no tile and are passed over).
+__device__ inline int tile_owner(const int32_t* first, int n, int k) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (first[mid] <= k) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+// The cached tokens of one row tile.  They are walked in steps of TT tokens:
+// first the sinks' [0, ns*TT), then the window's from lo on, both from
+// multiples of TT, so that no step is in both.
+struct TokenSpan {
+  int n, T, row0;        // sequence length, query tokens, first query row of the call
+  int lo, hi;            // the window part is [lo, hi), lo a multiple of TT
+  int ns, nt;            // steps of the sinks, steps in all
+  int per;               // steps of a split
+};
+
+template <int TT>
+__device__ inline TokenSpan token_span(const PagedView& v, const AttendArgs& a,
+                                       const AttendLists& s, int b, int tile, int row_tile) {
+  TokenSpan t;
+  const int hpg = v.H / v.G;
+  t.n = min(max(v.len[s.r.slot[b]], 0), v.cap);
+  t.row0 = s.r.row0[b];
+  t.T = s.r.row0[b + 1] - t.row0;
+  const int r0 = (tile - s.tile0[b]) * row_tile;
+  const int i0 = r0 / hpg, i1 = min((r0 + row_tile - 1) / hpg, t.T - 1);
+  int lo = 0, sinks = 0;
+  t.hi = t.n;
+  if (!a.mask) {
+    t.hi = min(t.n, max(t.n - t.T + i1 + 1, 0));
+    lo = max(t.n - t.T + i0 - a.window + 1, 0);
+    sinks = a.sinks;
+  }
+  t.lo = min(lo, t.hi) / TT * TT;
+  t.ns = (min(sinks, t.lo) + TT - 1) / TT;
+  t.nt = t.ns + (t.hi - t.lo + TT - 1) / TT;
+  // a split takes chunk tokens, or more where the lengths exceed the bound
+  // that the number of splits was made for
+  t.per = max((a.chunk + TT - 1) / TT, (t.nt + a.n_split - 1) / a.n_split);
+  return t;
+}
+
+// Token of step u's first.
+template <int TT>
+__device__ inline int step_token(const TokenSpan& t, int u) {
+  return u < t.ns ? u * TT : t.lo + (u - t.ns) * TT;
+}
+
+// The low k bits, k clamped to [0, 32].
+__device__ inline uint32_t low_bits(int k) {
+  return k >= 32 ? 0xFFFFFFFFu : k <= 0 ? 0u : (1u << k) - 1u;
+}
+
+// Which of the 32 cached tokens from t0 on query token i of the sequence
+// sees, bit by bit: those of a tree's mask, or of a window and the sinks.
+__device__ inline uint32_t seen_bits(const AttendArgs& a, const TokenSpan& s, int i, int t0) {
+  uint32_t in = low_bits(s.n - t0);
+  if (a.mask) {
+    const int j0 = t0 - (s.n - s.T);            // the first token's number among the drafted
+    const int j = max(j0, 0), w = j >> 6, sh = j & 63;
+    uint64_t m = 0;
+    if (j0 > -32 && w < a.words) {
+      const uint64_t* row = a.mask + (size_t)(s.row0 + i) * a.words + w;
+      m = row[0] >> sh;
+      if (sh > 32 && w + 1 < a.words) m |= row[1] << (64 - sh);
+    }
+    m &= low_bits(s.T - j);                     // bits behind the last drafted token
+    const int before = min(max(-j0, 0), 32);    // tokens before the drafted ones: all seen
+    return in & (low_bits(before) | (uint32_t)(m << before));
+  }
+  const int p = s.n - s.T + i;
+  in &= low_bits(p + 1 - t0);
+  return in & ~(low_bits(p - a.window + 1 - t0) & ~low_bits(a.sinks - t0));
+}
+
+// Whether every row i0..i1 sees every token of [t0, t0 + TT).
+template <int TT>
+__device__ inline bool all_see(const AttendArgs& a, const TokenSpan& s, int i0, int i1, int t0) {
+  const int p0 = s.n - s.T + i0, p1 = s.n - s.T + i1;
+  if (t0 + TT > s.n) return false;
+  if (a.mask) return t0 + TT <= s.n - s.T;
+  return t0 + TT - 1 <= p0 && (t0 > p1 - a.window || t0 + TT <= a.sinks);
+}
+
+// Columns [c, c + 4) of a finished row: o / l in the cache's type, and the
+// row's log-sum-exp (from its first columns' thread).
+template <typename T>
+__device__ inline void store_row(const AttendArgs& a, const PagedView& v, int layer, int g, int hpg,
+                                 int row0, int r, int c, float M, float L, f32x4 O) {
+  const size_t row = ((size_t)layer * a.n_rows + row0 + r / hpg) * v.H + g * hpg + r % hpg;
+  const bool none = M == -INFINITY && L == 0.f;     // the row sees nothing
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  T4 o;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] = (T)(none ? 0.f : O[j] / L);
+  *reinterpret_cast<T4*>(a.out + (row * v.d + c) * sizeof(T)) = o;
+  if (c == 0 && a.lse) a.lse[row] = none ? -INFINITY : fmaf(M, a.scale, __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
+}
+
+}  // namespace starkv
