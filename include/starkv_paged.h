@@ -47,7 +47,7 @@ extern "C" {
  *   page_tokens a power of two in [16, 1024], n_pages in [1, 2^26],
  *   n_slots in [1, 2^20], max_pages*page_tokens <= 2^26,
  *   strides times the element size multiples of 16 bytes, not negative,
- *   token_stride >= d; k and v 16-byte aligned, the int32 arrays 4-byte.
+ *   token_stride >= d and under 2^28 bytes; k and v 16-byte aligned, the int32 arrays 4-byte.
  * refs[p] is how many table entries name page p; a page is free when refs[p]
  * is 0.  Calls that allocate take the lowest-numbered pages that were free
  * when the call began, in the order of the call's sequences.  For one layer

@@ -15,7 +15,7 @@ LIB = os.path.join(PKG, "libstarkv.so")
 INCLUDE = os.path.join(ROOT, "include")
 
 HIP_SOURCES = ["score.hip", "score_bf16.hip", "score_f32.hip", "state.hip", "select.hip",
-               "compact.hip", "decode.hip", "noalloc.hip", "pages.hip", "attend.hip"]
+               "compact.hip", "decode.hip", "noalloc.hip", "pages.hip", "attend.hip", "attend_many.hip"]
 HOST_SOURCES = ["validate.cpp", "api.cpp", "paged_api.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -20,6 +20,13 @@ struct AttendArgs {
   float scale;            // log2(e) / sqrt(d)
 };
 
+// Tables and lengths do not change while a kernel reads them: uniform reads go
+// through the scalar cache.
+typedef __attribute__((address_space(4))) int32_t const_i32;
+__device__ inline const const_i32* const_ints(const int32_t* p) {
+  return (const const_i32*)(uintptr_t)p;
+}
+
 struct AttendLists {      // with PagedView and AttendArgs below 4 KB of kernel arguments
   RowList r;
   int32_t tile0[kMaxSeqs + 1];
@@ -52,7 +59,7 @@ __device__ inline TokenSpan token_span(const PagedView& v, const AttendArgs& a,
                                        const AttendLists& s, int b, int tile, int row_tile) {
   TokenSpan t;
   const int hpg = v.H / v.G;
-  t.n = min(max(v.len[s.r.slot[b]], 0), v.cap);
+  t.n = min(max(const_ints(v.len)[s.r.slot[b]], 0), v.cap);
   t.row0 = s.r.row0[b];
   t.T = s.r.row0[b + 1] - t.row0;
   const int r0 = (tile - s.tile0[b]) * row_tile;
@@ -115,19 +122,32 @@ __device__ inline bool all_see(const AttendArgs& a, const TokenSpan& s, int i0, 
   return t0 + TT - 1 <= p0 && (t0 > p1 - a.window || t0 + TT <= a.sinks);
 }
 
-// Columns [c, c + 4) of a finished row: o / l in the cache's type, and the
-// row's log-sum-exp (from its first columns' thread).
+// Columns [c, c + 4) of a finished row (of [n_layers][n_rows][H]): o / l in
+// the cache's type, and with its first columns the row's log-sum-exp.
+template <typename T>
+__device__ inline void store_out(const AttendArgs& a, int d, size_t row, int c, float M, float L,
+                                 f32x4 O) {
+  const bool none = M == -INFINITY && L == 0.f;     // the row sees nothing
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  T4 o;
+  const float inv = none ? 0.f : 1.f / L;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] = (T)(O[j] * inv);
+  *reinterpret_cast<T4*>(a.out + (row * d + c) * sizeof(T)) = o;
+  if (c == 0 && a.lse)
+    a.lse[row] = none ? -INFINITY : fmaf(M, a.scale, __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
+}
+
+// The same of row r of a (sequence, group) whose first query row is row0.
 template <typename T>
 __device__ inline void store_row(const AttendArgs& a, const PagedView& v, int layer, int g, int hpg,
                                  int row0, int r, int c, float M, float L, f32x4 O) {
   const size_t row = ((size_t)layer * a.n_rows + row0 + r / hpg) * v.H + g * hpg + r % hpg;
-  const bool none = M == -INFINITY && L == 0.f;     // the row sees nothing
-  typedef T T4 __attribute__((ext_vector_type(4)));
-  T4 o;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) o[j] = (T)(none ? 0.f : O[j] / L);
-  *reinterpret_cast<T4*>(a.out + (row * v.d + c) * sizeof(T)) = o;
-  if (c == 0 && a.lse) a.lse[row] = none ? -INFINITY : fmaf(M, a.scale, __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
+  store_out<T>(a, v.d, row, c, M, L, O);
 }
+
+// The kernel for many rows (attend_many.hip); the splits are joined after it.
+int launch_attend_many(const PagedView& v, const AttendArgs& a, const AttendLists& l,
+                       const AttendShape& s, hipStream_t st);
 
 }  // namespace starkv

@@ -163,7 +163,7 @@ __global__ __launch_bounds__(kThreads) void attend_few(PagedView v, AttendArgs a
     for (int t = 0; t < ND; ++t) o[nb][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  const int32_t* __restrict__ table = v.table + (size_t)s.r.slot[b] * v.max_pages;
+  const const_i32* table = const_ints(v.table + (size_t)s.r.slot[b] * v.max_pages);
   const int64_t base = (int64_t)layer * v.ls + (int64_t)g * v.gs;
   const int u1 = min((split + 1) * ts.per, ts.nt);
   for (int u = split * ts.per + wave; u < u1; u += kWaves) {
@@ -392,11 +392,19 @@ template <typename T, int D>
 int launch(const PagedView& v, const AttendArgs& a, const AttendLists& l, const AttendShape& s,
            hipStream_t st) {
   const unsigned blocks = (unsigned)(s.units * s.n_split);
-  if (s.row_tile == 16) attend_few<T, D, 1><<<blocks, kThreads, 0, st>>>(v, a, l);
-  else attend_few<T, D, 2><<<blocks, kThreads, 0, st>>>(v, a, l);
+  if (s.many) {
+    const int err = launch_attend_many(v, a, l, s, st);
+    if (err) return err;
+  } else if (s.row_tile == 16) {
+    attend_few<T, D, 1><<<blocks, kThreads, 0, st>>>(v, a, l);
+  } else {
+    attend_few<T, D, 2><<<blocks, kThreads, 0, st>>>(v, a, l);
+  }
   if (s.n_split > 1) {
     const int steps = s.row_tile / (kThreads / (D / 4));
-    attend_join<T, D, kStep><<<(unsigned)(s.units * steps), kThreads, 0, st>>>(v, a, l, s.row_tile);
+    const unsigned joins = (unsigned)(s.units * steps);
+    if (s.many) attend_join<T, D, 64><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile);
+    else attend_join<T, D, kStep><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile);
   }
   return (int)hipGetLastError();
 }

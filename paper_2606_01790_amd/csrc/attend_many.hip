@@ -1,0 +1,359 @@
+// Attention over the pages of a cache for many query rows (bf16): a tree of
+// several tokens, or a chunk of a prefill.  The rows of a (sequence, group)
+// share its K and V, so the pass is bound by the matrix units, or by HBM
+// where the rows are few.
+//
+// A block takes up to 256 rows, 32 for each of its waves, and walks the
+// tokens in steps of 64 that all its waves read from LDS, while the next
+// step's K and V travel from HBM straight to the other half of LDS.  As in
+// the kernel for few rows the tokens are on the A side of both products:
+//   S^T = K Q^T   on 32x32x16 MFMAs: a lane gets 16 tokens of each half of the
+//                 step for one row, so a row's maximum and sum stay in two lanes;
+//   O^T = V^T P^T the lane's weights are its part of B as they are (k = 8*half
+//                 + j stands for token 4*half + j or 8 + 4*half + j - 4 of 16),
+//                 and A's four tokens of a column come from LDS transposed.
+// The running maximum is only moved when a row's grows by more than 2^8: until
+// then the weights, up to 2^8, lose nothing, and the output need not be
+// rescaled.
+#include "attend.h"
+
+namespace starkv {
+namespace {
+
+constexpr int kMaxWaves = 8;
+constexpr int kStep = 64;
+constexpr int kGroups = kStep / 16;      // 16-token groups of a step: one page each
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+__device__ inline float both_halves_max(float v) {
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+__device__ inline float both_halves_sum(float v) {
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+}
+
+// Where 16-byte piece c of a token's row lies in LDS: the pieces of a row are
+// permuted by the token, so that the lanes of a read, which differ in the
+// token, meet different banks.  K is read one piece per token, V two
+// neighbouring ones of four tokens.
+template <int D>
+__device__ inline int k_swizzle(int token) {
+  return D == 128 ? token & 15 : (token >> 1) & 7;
+}
+template <int D>
+__device__ inline int v_swizzle(int token) {
+  return D == 128 ? (token & 7) * 2 : ((token >> 1) & 3) * 2;
+}
+
+// One 16-token group's K or V rows into LDS, 1 KB per instruction: lane i of
+// an instruction fills 16 bytes, piece i % NP of row i / NP, with the piece
+// that belongs there.  `piece` is that piece for the instruction's first
+// rows, `turn` what the rows before an instruction's first add to it.
+template <int D>
+__device__ inline void stage(const char* from, int64_t ts, int piece, int turn, uint32_t row,
+                             char* to) {
+  constexpr int kLoads = 16 * D * 2 / 1024, kRows = 16 / kLoads;
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const uint32_t off = row + (uint32_t)((piece ^ (turn * j & (D / 8 - 1))) << 4);
+    __builtin_amdgcn_global_load_lds(
+        (const __attribute__((address_space(1))) void*)(from + j * kRows * ts + off),
+        (__attribute__((address_space(3))) void*)(to + j * 1024), 16, 0, 0);
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, AttendArgs a,
+                                                                 AttendLists s) {
+  constexpr int NF = D / 16;               // k-steps of S
+  constexpr int ND = D / 32;               // 32-column tiles of the output
+  constexpr int kRow = D * 2;              // bytes of a row
+  constexpr int kLoads = 16 * kRow / 1024, kLoadRows = 16 / kLoads, NP = kRow / 16;
+  __shared__ __align__(1024) char k0[kStep * kRow], k1[kStep * kRow];
+  __shared__ __align__(1024) char v0[kStep * kRow], v1[kStep * kRow];
+
+  const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves = blockDim.x >> 6, row_tile = waves * 32;
+  // tiles of one split of a (layer, group) follow each other: they read the
+  // same K and V
+  const int tile = blockIdx.x % a.n_tiles;
+  const int split = blockIdx.x / a.n_tiles % a.n_split;
+  const int lg = blockIdx.x / a.n_tiles / a.n_split;
+  const int g = lg % v.G, layer = lg / v.G;
+  const int b = tile_owner(s.tile0, s.r.n, tile);
+  const TokenSpan ts = token_span<kStep>(v, a, s, b, tile, row_tile);
+  const int live = (ts.nt + ts.per - 1) / ts.per;
+  if (split >= max(live, 1)) return;
+  const int hpg = v.H / v.G;
+  const int rows = ts.T * hpg;
+  const int r0 = (tile - s.tile0[b]) * row_tile + wave * 32;
+  // a wave whose rows all lie behind the last only helps to load
+  const bool idle = r0 >= rows;
+  const int r = min(r0 + l32, rows - 1);
+  const int qi = r / hpg;
+  const int i0 = min(r0, rows - 1) / hpg, i1 = min(r0 + 31, rows - 1) / hpg;
+  const size_t out_row = ((size_t)layer * a.n_rows + ts.row0 + qi) * v.H + g * hpg + r % hpg;
+
+  bf16x8 qf[NF];
+#pragma unroll
+  for (int f = 0; f < NF; ++f)
+    qf[f] = *reinterpret_cast<const bf16x8*>(a.q + out_row * kRow + 32 * f + 16 * half);
+
+  // the lane's row and pieces of a staged group; the swizzles of tokens
+  // j*kLoadRows + i are those of j*kLoadRows and i combined by xor
+  const int sub = lane / NP;
+  const uint32_t row_off = (uint32_t)sub * (uint32_t)v.ts;
+  const int kpiece = (lane % NP) ^ k_swizzle<D>(sub), vpiece = (lane % NP) ^ v_swizzle<D>(sub);
+
+  const const_i32* table = const_ints(v.table + (size_t)s.r.slot[b] * v.max_pages);
+  const int64_t base = (int64_t)layer * v.ls + (int64_t)g * v.gs;
+  const int u0 = split * ts.per, u1 = min(u0 + ts.per, ts.nt);
+  const int bi0 = min((r0 - wave * 32) / hpg, ts.T - 1);       // query tokens of the block
+  const int bi1 = min(r0 - wave * 32 + row_tile - 1, rows - 1) / hpg;
+
+  // the pages of a step's groups, two to a word, read a step before their use
+  struct Pages { uint64_t lo, hi; };
+  static_assert(kGroups == 4, "two words of two pages");
+  const auto pages_at = [&](int u) {
+    const int t0 = step_token<kStep>(ts, min(u, ts.nt - 1));
+    const auto two = [&](int t) {
+      return (uint64_t)(uint32_t)table[min(t, ts.n - 1) >> v.psh] |
+             (uint64_t)(uint32_t)table[min(t + 16, ts.n - 1) >> v.psh] << 32;
+    };
+    return Pages{two(t0), two(t0 + 32)};
+  };
+  const auto page_of = [&](const Pages& p, int grp) {
+    return (int)((grp & 2 ? p.hi : p.lo) >> (32 * (grp & 1)));
+  };
+  // A step's jobs, one per 16-token group of K and one of V, dealt to the waves
+  const auto load_step = [&](int u, const Pages& p, char* kd, char* vd) {
+    const int t0 = step_token<kStep>(ts, u);
+    for (int job = wave; job < 2 * kGroups; job += waves) {
+      const int grp = job >> 1;
+      int page = page_of(p, grp);
+      if (page < 0 || page >= v.n_pages) page = 0;     // masked in the step
+      const int64_t from = base + (int64_t)page * v.ps +
+                           (int64_t)((t0 + 16 * grp) & (v.P - 1)) * v.ts;
+      const bool is_v = job & 1;
+      stage<D>((is_v ? v.v : v.k) + from, v.ts, is_v ? vpiece : kpiece,
+               is_v ? v_swizzle<D>(kLoadRows) : k_swizzle<D>(kLoadRows), row_off,
+               (is_v ? vd : kd) + grp * 16 * kRow);
+    }
+  };
+
+  float m = -INFINITY, l = 0.f;       // reference of the weights; this lane's part of the sum
+  f32x16 o[ND];
+#pragma unroll
+  for (int t = 0; t < ND; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
+
+  // One step on one half of LDS, while the next one's rows fill the other.
+  Pages now, next, later;
+  const auto step = [&](int u, char* ks, char* vs, char* kn, char* vn) {
+    // the step's loads are complete, and every wave is done with the step
+    // before, whose half of LDS the next loads fill
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    __syncthreads();
+    if (u + 1 < u1) load_step(u + 1, next, kn, vn);
+    later = pages_at(u + 2);
+
+    const int t0 = step_token<kStep>(ts, u);
+    // the tokens of the step that lie in a page, the same for the whole block
+    uint64_t held = 0;
+#pragma unroll
+    for (int grp = 0; grp < kGroups; ++grp) {
+      const int page = page_of(now, grp);
+      if (page >= 0 && page < v.n_pages) held |= (uint64_t)0xFFFF << (16 * grp);
+    }
+    now = next;
+    next = later;
+    held &= (uint64_t)low_bits(ts.n - t0) | (uint64_t)low_bits(ts.n - t0 - 32) << 32;
+    bool odd = false;
+    if (held != ~0ull || !all_see<kStep>(a, ts, bi0, bi1, t0)) {
+      // some rows do not see all of it.  What no page holds counts as zero;
+      // infinities and NaN of V need the way below
+      for (int i = threadIdx.x; i < kStep * NP; i += blockDim.x) {
+        const int token = i / NP;
+        u32x4* at = reinterpret_cast<u32x4*>(vs + i * 16);
+        if (!(held >> token & 1)) {
+          *at = u32x4{0, 0, 0, 0};
+        } else {
+          const u32x4 w = *at;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            odd |= (w[c] & 0x7F80u) == 0x7F80u || (w[c] & 0x7F800000u) == 0x7F800000u;
+        }
+      }
+      odd = __syncthreads_or(odd);
+    }
+
+    f32x16 x[2];
+    uint32_t seen[2] = {~0u, ~0u};
+    if (!idle) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          const int token = 32 * h + l32;
+          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(
+              ks + token * kRow + ((2 * f + half) ^ k_swizzle<D>(token)) * 16);
+          x[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[f], f ? x[h] : f32x16{}, 0, 0, 0);
+        }
+      if (held != ~0ull || !all_see<kStep>(a, ts, i0, i1, t0)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          seen[h] = (uint32_t)(held >> (32 * h)) & seen_bits(a, ts, qi, t0 + 32 * h);
+          const uint32_t mine = seen[h] >> (4 * half);
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            x[h][e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? x[h][e] : -INFINITY;
+        }
+      }
+      // the weights, against the row's reference
+      float mt = -INFINITY;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mt = fmaxf(mt, x[h][e]);
+      mt = both_halves_max(mt);
+      const bool grows = mt > m && (m == -INFINITY || (mt - m) * a.scale > 8.f);
+      if (__any(grows)) {
+        const float mn = grows ? mt : m;
+        const float alpha = mn == m ? 1.f : __builtin_amdgcn_exp2f((m - mn) * a.scale);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int t = 0; t < ND; ++t) o[t] *= alpha;
+      }
+      const float mf = m == -INFINITY ? 0.f : m, ms = mf * a.scale;
+      if (__any(!(fabsf(ms) < 1048576.f))) {
+        // a reference whose product with the scale has no places left for the
+        // differences: they are taken first
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[h][e] = __builtin_amdgcn_exp2f((x[h][e] - mf) * a.scale);
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            x[h][e] = __builtin_amdgcn_exp2f(fmaf(x[h][e], a.scale, -ms));
+      }
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum[h] += x[h][e];
+      l += sum[0] + sum[1];
+    }
+    if (odd) {
+      // infinities and NaN that some rows see and some do not: they are added
+      // token by token to the rows that see them, and are zero from then on
+      if (!idle) {
+        for (int token = 0; token < kStep; ++token) {
+          const int want = (token & 31) >> 3 << 2 | (token & 3) | token >> 5 << 4;
+          float w = 0.f;
+#pragma unroll
+          for (int k = 0; k < 32; ++k) w = k == want ? x[k >> 4][k & 15] : w;
+          w = __shfl(w, (token >> 2 & 1) * 32 + l32);
+          const bool sees_it = (token < 32 ? seen[0] : seen[1]) >> (token & 31) & 1;
+#pragma unroll
+          for (int t = 0; t < ND; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int col = 32 * t + 8 * (e >> 2) + 4 * half + (e & 3);
+              const float val = (float)*reinterpret_cast<const __bf16*>(
+                  vs + token * kRow + ((col >> 3) ^ v_swizzle<D>(token)) * 16 + (col & 7) * 2);
+              if (sees_it && !(fabsf(val) < INFINITY)) o[t][e] = fmaf(w, val, o[t][e]);
+            }
+        }
+      }
+      __syncthreads();
+      for (int i = threadIdx.x; i < kStep * NP; i += blockDim.x) {
+        u32x4 w = *reinterpret_cast<u32x4*>(vs + i * 16);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          if ((w[c] & 0x7F80u) == 0x7F80u) w[c] &= 0xFFFF0000u;
+          if ((w[c] & 0x7F800000u) == 0x7F800000u) w[c] &= 0xFFFFu;
+        }
+        *reinterpret_cast<u32x4*>(vs + i * 16) = w;
+      }
+      __syncthreads();
+    }
+    if (idle) return;
+    const int quad = lane >> 4 & 1, i = lane & 15;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      // tokens 16 k.. of the step; the weights rounded to bf16, V's type:
+      // half a step of 2^-8 each, below the rounding of the output
+      bf16x8 pf;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) pf[j] = (__bf16)x[k >> 1][8 * (k & 1) + j];
+#pragma unroll
+      for (int t = 0; t < ND; ++t) {
+        s16x4 got[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int token = 16 * k + 8 * h + 4 * half + (i >> 2);
+          const int piece = 4 * t + 2 * quad + (i >> 1 & 1);
+          got[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4*)(
+                  vs + token * kRow + (piece ^ v_swizzle<D>(token)) * 16 + (i & 1) * 8));
+        }
+        const s16x8 vf = __builtin_shufflevector(got[0], got[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), pf, o[t], 0, 0, 0);
+      }
+    }
+  };
+
+  if (u0 < u1) {
+    now = pages_at(u0);
+    next = pages_at(u0 + 1);
+    load_step(u0, now, k0, v0);
+  }
+  for (int u = u0; u < u1; u += 2) {
+    step(u, k0, v0, k1, v1);
+    if (u + 1 < u1) step(u + 1, k1, v1, k0, v0);
+  }
+
+  l = both_halves_sum(l);
+  if (idle || r0 + l32 >= rows) return;
+  if (live > 1) {
+    const size_t unit = (size_t)lg * a.n_tiles + tile;
+    const size_t rec = (unit * a.n_split + split) * row_tile + wave * 32 + l32;
+#pragma unroll
+    for (int t = 0; t < ND; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(a.part + rec * D + 32 * t + 8 * i + 4 * half) =
+            f32x4{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
+    if (half == 0) a.stat[rec] = float2{m, l};
+    return;
+  }
+#pragma unroll
+  for (int t = 0; t < ND; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      store_out<__bf16>(a, v.d, out_row, 32 * t + 8 * i + 4 * half, m, l,
+                        f32x4{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]});
+}
+
+}  // namespace
+
+int launch_attend_many(const PagedView& v, const AttendArgs& a, const AttendLists& l,
+                       const AttendShape& s, hipStream_t st) {
+  const unsigned blocks = (unsigned)(s.units * s.n_split), threads = (unsigned)(s.row_tile * 2);
+  if (v.d == 128) attend_many<128><<<blocks, threads, 0, st>>>(v, a, l);
+  else attend_many<64><<<blocks, threads, 0, st>>>(v, a, l);
+  return (int)hipGetLastError();
+}
+
+}  // namespace starkv

@@ -70,6 +70,7 @@ int launch_pages_compact(const PagedView& v, const SeqList& s, bool whole, const
 // are its tokens' heads of the group, r = i*(H/G) + head; a block takes a
 // tile of row_tile of them and one split of the cached tokens.
 struct AttendShape {
+  bool many;        // the kernel for many rows
   int n_rows;       // query tokens of the call
   int row_tile;     // rows of a block
   int n_tiles;      // row tiles of one (layer, group), over all sequences

@@ -35,6 +35,7 @@ starkv_status check_paged(const starkv_paged* c, PagedView* v) {
     if (s < 0 || s > INT64_MAX / 8) return STARKV_E_SHAPE;
     if (s * esz % 16) return STARKV_E_ALIGN;
   }
+  if (c->token_stride * esz >= 1 << 28) return STARKV_E_SHAPE;   // 32-bit offsets within 8 rows
   if (!c->k || !c->v || !c->table || !c->len || !c->refs) return STARKV_E_NULL;
   if (!at(c->k, 16) || !at(c->v, 16) || !at(c->table, 4) || !at(c->len, 4) || !at(c->refs, 4))
     return STARKV_E_ALIGN;
@@ -125,7 +126,15 @@ starkv_status attend_shape(const PagedView& v, const int32_t* rows, int n, int32
   }
   if (tot > kMaxTokens) return STARKV_E_PARAM;
   s->n_rows = (int)tot;
-  s->row_tile = most * hpg <= 16 ? 16 : 32;
+  const int64_t R = most * hpg;
+  s->many = v.esz == 2 && R > 32;
+  if (s->many) {
+    // equal row tiles of whole 32-row waves, at most eight of them
+    const int64_t parts = (R + 255) / 256;
+    s->row_tile = (int)((R + 32 * parts - 1) / (32 * parts) * 32);
+  } else {
+    s->row_tile = R <= 16 ? 16 : 32;
+  }
   int64_t tiles = 0;
   for (int b = 0; b < n; ++b) {
     if (tile0) tile0[b] = (int32_t)tiles;

@@ -66,7 +66,7 @@ def test_constants_match_the_header():
     (dict(n_pages=0), "E_SHAPE"), (dict(n_slots=0), "E_SHAPE"), (dict(max_pages=0), "E_SHAPE"),
     (dict(max_pages=1 << 21), "E_SHAPE"), (dict(reserved=1), "E_SHAPE"),
     (dict(token_stride=120), "E_SHAPE"), (dict(token_stride=132), "E_ALIGN"),
-    (dict(page_stride=-8), "E_SHAPE"), (dict(group_stride=4), "E_ALIGN"),
+    (dict(token_stride=1 << 27), "E_SHAPE"), (dict(page_stride=-8), "E_SHAPE"), (dict(group_stride=4), "E_ALIGN"),
     (dict(k=None), "E_NULL"), (dict(refs=None), "E_NULL"), (dict(v=FAKE + 8), "E_ALIGN"),
     (dict(table=FAKE + 2), "E_ALIGN"),
 ])
