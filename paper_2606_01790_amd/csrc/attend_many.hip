@@ -117,26 +117,22 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, At
   const int bi0 = min((r0 - wave * 32) / hpg, ts.T - 1);       // query tokens of the block
   const int bi1 = min(r0 - wave * 32 + row_tile - 1, rows - 1) / hpg;
 
-  // the pages of a step's groups, two to a word, read a step before their use
-  struct Pages { uint64_t lo, hi; };
+  // the pages of half a step's two groups, read a step before their use
   static_assert(kGroups == 4, "two words of two pages");
-  const auto pages_at = [&](int u) {
-    const int t0 = step_token<kStep>(ts, min(u, ts.nt - 1));
-    const auto two = [&](int t) {
-      return (uint64_t)(uint32_t)table[min(t, ts.n - 1) >> v.psh] |
-             (uint64_t)(uint32_t)table[min(t + 16, ts.n - 1) >> v.psh] << 32;
-    };
-    return Pages{two(t0), two(t0 + 32)};
+  const auto two_pages = [&](int u, int h) {
+    const int t = step_token<kStep>(ts, min(u, ts.nt - 1)) + 32 * h;
+    return (uint64_t)(uint32_t)table[min(t, ts.n - 1) >> v.psh] |
+           (uint64_t)(uint32_t)table[min(t + 16, ts.n - 1) >> v.psh] << 32;
   };
-  const auto page_of = [&](const Pages& p, int grp) {
-    return (int)((grp & 2 ? p.hi : p.lo) >> (32 * (grp & 1)));
+  const auto page_of = [](uint64_t lo, uint64_t hi, int grp) {
+    return (int)((grp & 2 ? hi : lo) >> (32 * (grp & 1)));
   };
   // A step's jobs, one per 16-token group of K and one of V, dealt to the waves
-  const auto load_step = [&](int u, const Pages& p, char* kd, char* vd) {
+  const auto load_step = [&](int u, uint64_t lo, uint64_t hi, char* kd, char* vd) {
     const int t0 = step_token<kStep>(ts, u);
     for (int job = wave; job < 2 * kGroups; job += waves) {
       const int grp = job >> 1;
-      int page = page_of(p, grp);
+      int page = page_of(lo, hi, grp);
       if (page < 0 || page >= v.n_pages) page = 0;     // masked in the step
       const int64_t from = base + (int64_t)page * v.ps +
                            (int64_t)((t0 + 16 * grp) & (v.P - 1)) * v.ts;
@@ -155,25 +151,27 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, At
     for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
 
   // One step on one half of LDS, while the next one's rows fill the other.
-  Pages now, next, later;
+  uint64_t now_lo = 0, now_hi = 0, next_lo = 0, next_hi = 0;
   const auto step = [&](int u, char* ks, char* vs, char* kn, char* vn) {
     // the step's loads are complete, and every wave is done with the step
     // before, whose half of LDS the next loads fill
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     __syncthreads();
-    if (u + 1 < u1) load_step(u + 1, next, kn, vn);
-    later = pages_at(u + 2);
+    if (u + 1 < u1) load_step(u + 1, next_lo, next_hi, kn, vn);
+    const uint64_t later_lo = two_pages(u + 2, 0), later_hi = two_pages(u + 2, 1);
 
     const int t0 = step_token<kStep>(ts, u);
     // the tokens of the step that lie in a page, the same for the whole block
     uint64_t held = 0;
 #pragma unroll
     for (int grp = 0; grp < kGroups; ++grp) {
-      const int page = page_of(now, grp);
+      const int page = page_of(now_lo, now_hi, grp);
       if (page >= 0 && page < v.n_pages) held |= (uint64_t)0xFFFF << (16 * grp);
     }
-    now = next;
-    next = later;
+    now_lo = next_lo;
+    now_hi = next_hi;
+    next_lo = later_lo;
+    next_hi = later_hi;
     held &= (uint64_t)low_bits(ts.n - t0) | (uint64_t)low_bits(ts.n - t0 - 32) << 32;
     bool odd = false;
     if (held != ~0ull || !all_see<kStep>(a, ts, bi0, bi1, t0)) {
@@ -197,15 +195,28 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, At
     f32x16 x[2];
     uint32_t seen[2] = {~0u, ~0u};
     if (!idle) {
+      bf16x8 kf[2][NF];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int f = 0; f < NF; ++f)
 #pragma unroll
-        for (int f = 0; f < NF; ++f) {
+        for (int h = 0; h < 2; ++h) {
           const int token = 32 * h + l32;
-          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(
+          kf[h][f] = *reinterpret_cast<const bf16x8*>(
               ks + token * kRow + ((2 * f + half) ^ k_swizzle<D>(token)) * 16);
-          x[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[f], f ? x[h] : f32x16{}, 0, 0, 0);
         }
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          x[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[h][f], qf[f], f ? x[h] : f32x16{}, 0, 0, 0);
+      // six fragments ahead of the products, then one for one
+      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+      for (int f = 0; f < 2 * NF - 6; ++f) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
       if (held != ~0ull || !all_see<kStep>(a, ts, i0, i1, t0)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -290,13 +301,14 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, At
     }
     if (idle) return;
     const int quad = lane >> 4 & 1, i = lane & 15;
+    s16x8 vf[4][ND];
+    bf16x8 pf[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       // tokens 16 k.. of the step; the weights rounded to bf16, V's type:
       // half a step of 2^-8 each, below the rounding of the output
-      bf16x8 pf;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) pf[j] = (__bf16)x[k >> 1][8 * (k & 1) + j];
+      for (int j = 0; j < 8; ++j) pf[k][j] = (__bf16)x[k >> 1][8 * (k & 1) + j];
 #pragma unroll
       for (int t = 0; t < ND; ++t) {
         s16x4 got[2];
@@ -308,16 +320,30 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, At
               (__attribute__((address_space(3))) s16x4*)(
                   vs + token * kRow + (piece ^ v_swizzle<D>(token)) * 16 + (i & 1) * 8));
         }
-        const s16x8 vf = __builtin_shufflevector(got[0], got[1], 0, 1, 2, 3, 4, 5, 6, 7);
-        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), pf, o[t], 0, 0, 0);
+        vf[k][t] = __builtin_shufflevector(got[0], got[1], 0, 1, 2, 3, 4, 5, 6, 7);
       }
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int t = 0; t < ND; ++t)
+        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[k][t]), pf[k], o[t],
+                                                       0, 0, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 12, 1);
+#pragma unroll
+    for (int f = 0; f < 4 * ND - 6; ++f) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 6, 1);
   };
 
   if (u0 < u1) {
-    now = pages_at(u0);
-    next = pages_at(u0 + 1);
-    load_step(u0, now, k0, v0);
+    now_lo = two_pages(u0, 0);
+    now_hi = two_pages(u0, 1);
+    next_lo = two_pages(u0 + 1, 0);
+    next_hi = two_pages(u0 + 1, 1);
+    load_step(u0, now_lo, now_hi, k0, v0);
   }
   for (int u = u0; u < u1; u += 2) {
     step(u, k0, v0, k1, v1);
