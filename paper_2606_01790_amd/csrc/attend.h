@@ -113,13 +113,19 @@ __device__ inline uint32_t seen_bits(const AttendArgs& a, const TokenSpan& s, in
   return in & ~(low_bits(p - a.window + 1 - t0) & ~low_bits(a.sinks - t0));
 }
 
-// Whether every row i0..i1 sees every token of [t0, t0 + TT).
-template <int TT>
-__device__ inline bool all_see(const AttendArgs& a, const TokenSpan& s, int i0, int i1, int t0) {
+// The tokens that query tokens i0..i1 all see, but for dropped ones: [lo, hi),
+// and [0, sinks).
+struct AllSee {
+  int lo, hi, sinks;
+};
+__device__ inline AllSee all_see(const AttendArgs& a, const TokenSpan& s, int i0, int i1) {
+  if (a.mask) return AllSee{0, s.n - s.T, 0};
   const int p0 = s.n - s.T + i0, p1 = s.n - s.T + i1;
-  if (t0 + TT > s.n) return false;
-  if (a.mask) return t0 + TT <= s.n - s.T;
-  return t0 + TT - 1 <= p0 && (t0 > p1 - a.window || t0 + TT <= a.sinks);
+  return AllSee{p1 - a.window + 1, min(p0 + 1, s.n), min(a.sinks, p0 + 1)};
+}
+template <int TT>
+__device__ inline bool sees_step(const AllSee& w, int t0) {
+  return t0 + TT <= w.hi && (t0 >= w.lo || t0 + TT <= w.sinks);
 }
 
 // Columns [c, c + 4) of a finished row (of [n_layers][n_rows][H]): o / l in

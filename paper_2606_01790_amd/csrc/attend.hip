@@ -137,7 +137,7 @@ __global__ __launch_bounds__(kThreads) void attend_few(PagedView v, AttendArgs a
   const int hpg = v.H / v.G;
   const int r0 = (tile - s.tile0[b]) * kRows;
   const int rows = ts.T * hpg;
-  const int i0 = r0 / hpg, i1 = min(r0 + kRows - 1, rows - 1) / hpg;
+  const AllSee all = all_see(a, ts, r0 / hpg, min(r0 + kRows - 1, rows - 1) / hpg);
 
   // this lane's row of each 16-row block: query token qi (its rows past the
   // last repeat the last, and are not written)
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(kThreads) void attend_few(PagedView v, AttendArgs a
         for (int c = 0; c < VR::kLoads; ++c)
           vv[4 * h + j][c] = *reinterpret_cast<const vrow*>(vr + j * v.ts + 16 * sizeof(vrow) * c);
     }
-    const bool whole = there[0] && there[1] && all_see<kStep>(a, ts, i0, i1, t0);
+    const bool whole = there[0] && there[1] && sees_step<kStep>(all, t0);
 
     f32x4 x[NB][2];
 #pragma unroll

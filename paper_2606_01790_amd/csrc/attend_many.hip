@@ -3,7 +3,7 @@
 // share its K and V, so the pass is bound by the matrix units, or by HBM
 // where the rows are few.
 //
-// A block takes up to 256 rows, 32 for each of its waves, and walks the
+// A block takes up to 128 rows, 32 for each of its waves, and walks the
 // tokens in steps of 64 that all its waves read from LDS, while the next
 // step's K and V travel from HBM straight to the other half of LDS.  As in
 // the kernel for few rows the tokens are on the A side of both products:
@@ -15,12 +15,14 @@
 // The running maximum is only moved when a row's grows by more than 2^8: until
 // then the weights, up to 2^8, lose nothing, and the output need not be
 // rescaled.
+#include <algorithm>
+
 #include "attend.h"
 
 namespace starkv {
 namespace {
 
-constexpr int kMaxWaves = 8;
+constexpr int kMaxWaves = 4;
 constexpr int kStep = 64;
 constexpr int kGroups = kStep / 16;      // 16-token groups of a step: one page each
 
@@ -39,37 +41,41 @@ __device__ inline float both_halves_sum(float v) {
 
 // Where 16-byte piece c of a token's row lies in LDS: the pieces of a row are
 // permuted by the token, so that the lanes of a read, which differ in the
-// token, meet different banks.  K is read one piece per token, V two
-// neighbouring ones of four tokens.
+// token, meet different banks.  K is read one piece per token, V four
+// neighbouring ones of four tokens by half a wave.
 template <int D>
 __device__ inline int k_swizzle(int token) {
   return D == 128 ? token & 15 : (token >> 1) & 7;
 }
 template <int D>
 __device__ inline int v_swizzle(int token) {
-  return D == 128 ? (token & 7) * 2 : ((token >> 1) & 3) * 2;
+  return D == 128 ? (token & 3) * 4 : ((token >> 1) & 1) * 4;
 }
 
 // One 16-token group's K or V rows into LDS, 1 KB per instruction: lane i of
-// an instruction fills 16 bytes, piece i % NP of row i / NP, with the piece
-// that belongs there.  `piece` is that piece for the instruction's first
-// rows, `turn` what the rows before an instruction's first add to it.
+// instruction j fills 16 bytes, piece i % NP of row j*kRows + i / NP, with the
+// piece that belongs there, off[j] behind the group's first row.
 template <int D>
-__device__ inline void stage(const char* from, int64_t ts, int piece, int turn, uint32_t row,
-                             char* to) {
-  constexpr int kLoads = 16 * D * 2 / 1024, kRows = 16 / kLoads;
+__device__ inline void stage(const char* from, const uint32_t (&off)[16 * D * 2 / 1024], char* to) {
 #pragma unroll
-  for (int j = 0; j < kLoads; ++j) {
-    const uint32_t off = row + (uint32_t)((piece ^ (turn * j & (D / 8 - 1))) << 4);
-    __builtin_amdgcn_global_load_lds(
-        (const __attribute__((address_space(1))) void*)(from + j * kRows * ts + off),
-        (__attribute__((address_space(3))) void*)(to + j * 1024), 16, 0, 0);
-  }
+  for (int j = 0; j < 16 * D * 2 / 1024; ++j)
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + off[j]),
+                                     (__attribute__((address_space(3))) void*)(to + j * 1024), 16, 0,
+                                     0);
+}
+
+// Blocks are dealt to the 8 XCDs round-robin by number.  Work items that
+// follow each other share K and V: each XCD takes `run` of them in turn, so
+// that its L2 holds what they read, and all XCDs move through the items
+// together, whose costs differ from end to end.
+__device__ inline unsigned xcd_item(unsigned block, unsigned run) {
+  const unsigned xcd = block & 7, i = block >> 3;
+  return (i / run * 8 + xcd) * run + i % run;
 }
 
 template <int D>
 __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, AttendArgs a,
-                                                                 AttendLists s) {
+                                                                 AttendLists s, unsigned run) {
   constexpr int NF = D / 16;               // k-steps of S
   constexpr int ND = D / 32;               // 32-column tiles of the output
   constexpr int kRow = D * 2;              // bytes of a row
@@ -81,10 +87,12 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, At
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int waves = blockDim.x >> 6, row_tile = waves * 32;
   // tiles of one split of a (layer, group) follow each other: they read the
-  // same K and V
-  const int tile = blockIdx.x % a.n_tiles;
-  const int split = blockIdx.x / a.n_tiles % a.n_split;
-  const int lg = blockIdx.x / a.n_tiles / a.n_split;
+  // same K and V.  Later tiles, which may see more, come first
+  const unsigned item = xcd_item(blockIdx.x, run);
+  const int tile = a.n_tiles - 1 - item % a.n_tiles;
+  const int split = item / a.n_tiles % a.n_split;
+  const int lg = item / a.n_tiles / a.n_split;
+  if (lg >= v.n_layers * v.G) return;
   const int g = lg % v.G, layer = lg / v.G;
   const int b = tile_owner(s.tile0, s.r.n, tile);
   const TokenSpan ts = token_span<kStep>(v, a, s, b, tile, row_tile);
@@ -97,7 +105,9 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, At
   const bool idle = r0 >= rows;
   const int r = min(r0 + l32, rows - 1);
   const int qi = r / hpg;
-  const int i0 = min(r0, rows - 1) / hpg, i1 = min(r0 + 31, rows - 1) / hpg;
+  const AllSee mine = all_see(a, ts, min(r0, rows - 1) / hpg, min(r0 + 31, rows - 1) / hpg);
+  const int b0 = r0 - wave * 32;
+  const AllSee block = all_see(a, ts, b0 / hpg, min(b0 + row_tile - 1, rows - 1) / hpg);
   const size_t out_row = ((size_t)layer * a.n_rows + ts.row0 + qi) * v.H + g * hpg + r % hpg;
 
   bf16x8 qf[NF];
@@ -105,41 +115,34 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, At
   for (int f = 0; f < NF; ++f)
     qf[f] = *reinterpret_cast<const bf16x8*>(a.q + out_row * kRow + 32 * f + 16 * half);
 
-  // the lane's row and pieces of a staged group; the swizzles of tokens
-  // j*kLoadRows + i are those of j*kLoadRows and i combined by xor
-  const int sub = lane / NP;
-  const uint32_t row_off = (uint32_t)sub * (uint32_t)v.ts;
-  const int kpiece = (lane % NP) ^ k_swizzle<D>(sub), vpiece = (lane % NP) ^ v_swizzle<D>(sub);
+  // where the lane's 16 bytes of a staged group's loads lie
+  uint32_t koff[kLoads], voff[kLoads];
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const int token = j * kLoadRows + lane / NP, piece = lane % NP;
+    koff[j] = (uint32_t)token * (uint32_t)v.ts + (piece ^ k_swizzle<D>(token)) * 16;
+    voff[j] = (uint32_t)token * (uint32_t)v.ts + (piece ^ v_swizzle<D>(token)) * 16;
+  }
 
   const const_i32* table = const_ints(v.table + (size_t)s.r.slot[b] * v.max_pages);
   const int64_t base = (int64_t)layer * v.ls + (int64_t)g * v.gs;
   const int u0 = split * ts.per, u1 = min(u0 + ts.per, ts.nt);
-  const int bi0 = min((r0 - wave * 32) / hpg, ts.T - 1);       // query tokens of the block
-  const int bi1 = min(r0 - wave * 32 + row_tile - 1, rows - 1) / hpg;
-
   // the pages of half a step's two groups, read a step before their use
   static_assert(kGroups == 4, "two words of two pages");
-  const auto two_pages = [&](int u, int h) {
-    const int t = step_token<kStep>(ts, min(u, ts.nt - 1)) + 32 * h;
+  const auto two_pages = [&](int t) {
     return (uint64_t)(uint32_t)table[min(t, ts.n - 1) >> v.psh] |
            (uint64_t)(uint32_t)table[min(t + 16, ts.n - 1) >> v.psh] << 32;
   };
-  const auto page_of = [](uint64_t lo, uint64_t hi, int grp) {
-    return (int)((grp & 2 ? hi : lo) >> (32 * (grp & 1)));
-  };
-  // A step's jobs, one per 16-token group of K and one of V, dealt to the waves
+  // A step's 16-token groups are dealt to the waves
   const auto load_step = [&](int u, uint64_t lo, uint64_t hi, char* kd, char* vd) {
     const int t0 = step_token<kStep>(ts, u);
-    for (int job = wave; job < 2 * kGroups; job += waves) {
-      const int grp = job >> 1;
-      int page = page_of(lo, hi, grp);
-      if (page < 0 || page >= v.n_pages) page = 0;     // masked in the step
+    for (int grp = wave; grp < kGroups; grp += waves) {
+      int page = (int)((grp & 2 ? hi : lo) >> (32 * (grp & 1)));
+      if ((unsigned)page >= (unsigned)v.n_pages) page = 0;     // masked in the step
       const int64_t from = base + (int64_t)page * v.ps +
                            (int64_t)((t0 + 16 * grp) & (v.P - 1)) * v.ts;
-      const bool is_v = job & 1;
-      stage<D>((is_v ? v.v : v.k) + from, v.ts, is_v ? vpiece : kpiece,
-               is_v ? v_swizzle<D>(kLoadRows) : k_swizzle<D>(kLoadRows), row_off,
-               (is_v ? vd : kd) + grp * 16 * kRow);
+      stage<D>(v.k + from, koff, kd + grp * 16 * kRow);
+      stage<D>(v.v + from, voff, vd + grp * 16 * kRow);
     }
   };
 
@@ -157,24 +160,26 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, At
     // before, whose half of LDS the next loads fill
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     __syncthreads();
+    const int t2 = step_token<kStep>(ts, min(u + 2, ts.nt - 1));
+    const uint64_t later_lo = two_pages(t2), later_hi = two_pages(t2 + 32);
     if (u + 1 < u1) load_step(u + 1, next_lo, next_hi, kn, vn);
-    const uint64_t later_lo = two_pages(u + 2, 0), later_hi = two_pages(u + 2, 1);
+    // the page numbers are waited for here: scalar loads under way would make
+    // every wait for a fragment one for all of them
+    asm volatile("" ::"s"(later_lo), "s"(later_hi));
 
     const int t0 = step_token<kStep>(ts, u);
-    // the tokens of the step that lie in a page, the same for the whole block
-    uint64_t held = 0;
-#pragma unroll
-    for (int grp = 0; grp < kGroups; ++grp) {
-      const int page = page_of(now_lo, now_hi, grp);
-      if (page >= 0 && page < v.n_pages) held |= (uint64_t)0xFFFF << (16 * grp);
-    }
-    now_lo = next_lo;
-    now_hi = next_hi;
-    next_lo = later_lo;
-    next_hi = later_hi;
-    held &= (uint64_t)low_bits(ts.n - t0) | (uint64_t)low_bits(ts.n - t0 - 32) << 32;
+    const unsigned top_page = max(max((unsigned)now_lo, (unsigned)(now_lo >> 32)),
+                                  max((unsigned)now_hi, (unsigned)(now_hi >> 32)));
+    const bool all_pages = top_page < (unsigned)v.n_pages;
+    uint64_t held = ~0ull;       // the tokens of the step that lie in a page
     bool odd = false;
-    if (held != ~0ull || !all_see<kStep>(a, ts, bi0, bi1, t0)) {
+    if (!all_pages || !sees_step<kStep>(block, t0)) {
+#pragma unroll
+      for (int grp = 0; grp < kGroups; ++grp) {
+        const unsigned page = (unsigned)((grp & 2 ? now_hi : now_lo) >> (32 * (grp & 1)));
+        if (page >= (unsigned)v.n_pages) held &= ~((uint64_t)0xFFFF << (16 * grp));
+      }
+      held &= (uint64_t)low_bits(ts.n - t0) | (uint64_t)low_bits(ts.n - t0 - 32) << 32;
       // some rows do not see all of it.  What no page holds counts as zero;
       // infinities and NaN of V need the way below
       for (int i = threadIdx.x; i < kStep * NP; i += blockDim.x) {
@@ -191,6 +196,10 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, At
       }
       odd = __syncthreads_or(odd);
     }
+    now_lo = next_lo;
+    now_hi = next_hi;
+    next_lo = later_lo;
+    next_hi = later_hi;
 
     f32x16 x[2];
     uint32_t seen[2] = {~0u, ~0u};
@@ -217,7 +226,7 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, At
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
       __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
-      if (held != ~0ull || !all_see<kStep>(a, ts, i0, i1, t0)) {
+      if (!all_pages || !sees_step<kStep>(mine, t0)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           seen[h] = (uint32_t)(held >> (32 * h)) & seen_bits(a, ts, qi, t0 + 32 * h);
@@ -339,10 +348,11 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, At
   };
 
   if (u0 < u1) {
-    now_lo = two_pages(u0, 0);
-    now_hi = two_pages(u0, 1);
-    next_lo = two_pages(u0 + 1, 0);
-    next_hi = two_pages(u0 + 1, 1);
+    const int t0 = step_token<kStep>(ts, u0), t1 = step_token<kStep>(ts, min(u0 + 1, ts.nt - 1));
+    now_lo = two_pages(t0);
+    now_hi = two_pages(t0 + 32);
+    next_lo = two_pages(t1);
+    next_hi = two_pages(t1 + 32);
     load_step(u0, now_lo, now_hi, k0, v0);
   }
   for (int u = u0; u < u1; u += 2) {
@@ -376,9 +386,12 @@ __global__ __launch_bounds__(64 * kMaxWaves, 2) void attend_many(PagedView v, At
 
 int launch_attend_many(const PagedView& v, const AttendArgs& a, const AttendLists& l,
                        const AttendShape& s, hipStream_t st) {
-  const unsigned blocks = (unsigned)(s.units * s.n_split), threads = (unsigned)(s.row_tile * 2);
-  if (v.d == 128) attend_many<128><<<blocks, threads, 0, st>>>(v, a, l);
-  else attend_many<64><<<blocks, threads, 0, st>>>(v, a, l);
+  // the row tiles of a (layer, group) that one XCD takes at a time
+  const unsigned run = (unsigned)std::min(s.n_tiles, 4), items = (unsigned)(s.units * s.n_split);
+  const unsigned blocks = (items + 8 * run - 1) / (8 * run) * (8 * run);
+  const unsigned threads = (unsigned)(s.row_tile * 2);
+  if (v.d == 128) attend_many<128><<<blocks, threads, 0, st>>>(v, a, l, run);
+  else attend_many<64><<<blocks, threads, 0, st>>>(v, a, l, run);
   return (int)hipGetLastError();
 }
 
