@@ -129,9 +129,7 @@ starkv_status attend_shape(const PagedView& v, const int32_t* rows, int n, int32
   const int64_t R = most * hpg;
   s->many = v.esz == 2 && R > 32;
   if (s->many) {
-    // equal row tiles of whole 32-row waves, at most eight of them
-    const int64_t parts = (R + 127) / 128;
-    s->row_tile = (int)((R + 32 * parts - 1) / (32 * parts) * 32);
+    s->row_tile = R <= 64 ? 64 : 128;
   } else {
     s->row_tile = R <= 16 ? 16 : 32;
   }
