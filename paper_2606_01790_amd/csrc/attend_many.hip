@@ -101,13 +101,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
   const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   constexpr int row_tile = WAVES * 32;
-  // tiles of one split of a (layer, group) follow each other: they read the
-  // same K and V.  Later tiles, which may see more, come first
+  // `run` tiles of one split of a (layer, group) follow each other: they read
+  // the same K and V.  Later tiles, which may see more, come first, those of
+  // all (layer, group)s together
   const unsigned item = xcd_item(blockIdx.x, run);
-  const int tile = a.n_tiles - 1 - item % a.n_tiles;
-  const int split = item / a.n_tiles % a.n_split;
-  const int lg = item / a.n_tiles / a.n_split;
-  if (lg >= v.n_layers * v.G) return;
+  const unsigned lgs = v.n_layers * v.G, runs = (a.n_tiles + run - 1) / run, at_run = item / run;
+  const int lg = at_run % lgs, split = at_run / lgs / runs;
+  const int tile = a.n_tiles - 1 - (int)(at_run / lgs % runs * run + item % run);
+  if (split >= a.n_split || tile < 0) return;
   const int g = lg % v.G, layer = lg / v.G;
   const int b = tile_owner(s.tile0, s.r.n, tile);
   const TokenSpan ts = token_span<kStep>(v, a, s, b, tile, row_tile);
@@ -183,12 +184,18 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
   };
 
   float m = -INFINITY, l = 0.f;       // reference of the weights; this lane's part of the sum
+  float top = -INFINITY;              // the step's largest logit of the lane
   f32x16 o[ND], x[2];
 #pragma unroll
   for (int t = 0; t < ND; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
 
+  const auto quarter_max = [](const f32x16 (&z)[2], int q, float best) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) best = fmaxf(best, z[q >> 1][8 * (q & 1) + e]);
+    return best;
+  };
   // LDS offsets of the lane's fragments, the same in every buffer
   uint32_t kat[NF], vat[ND];
 #pragma unroll
@@ -267,14 +274,12 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
           for (int e = 0; e < 16; ++e)
             x[h][e] = bits >> (8 * (e >> 2) + (e & 3)) & 1 ? x[h][e] : -INFINITY;
         }
+        top = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) top = quarter_max(x, q, top);
       }
       // the weights, against the row's reference
-      float mt = -INFINITY;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) mt = fmaxf(mt, x[h][e]);
-      mt = both_halves_max(mt);
+      const float mt = both_halves_max(top);
       const bool grows = mt > m && (m == -INFINITY || (mt - m) * a.scale > 8.f);
       if (__any(grows)) {
         const float mn = grows ? mt : m;
@@ -398,6 +403,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
         o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k][t], pf, o[t], 0, 0, 0);
       }
       if (k == 1) look_ahead();
+      // the next step's largest logit, should all of it be seen
+      top = quarter_max(y, k, k ? top : -INFINITY);
       __builtin_amdgcn_sched_barrier(0);
     }
     x[0] = y[0];
@@ -427,6 +434,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
         for (int h = 0; h < 2; ++h)
           x[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(k0, f, h), qf[f], f ? x[h] : f32x16{}, 0,
                                                          0, 0);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) top = quarter_max(x, q, top);
     }
   }
   for (int u = u0; u < u1; u += 2) {
@@ -462,8 +471,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
 int launch_attend_many(const PagedView& v, const AttendArgs& a, const AttendLists& l,
                        const AttendShape& s, hipStream_t st) {
   // the row tiles of a (layer, group) that one XCD takes at a time
-  const unsigned run = (unsigned)std::min(s.n_tiles, 4), items = (unsigned)(s.units * s.n_split);
-  const unsigned blocks = (items + 8 * run - 1) / (8 * run) * (8 * run);
+  const unsigned run = (unsigned)std::min(s.n_tiles, 4);
+  const unsigned runs = (unsigned)((s.n_tiles + run - 1) / run) * v.n_layers * v.G * s.n_split;
+  const unsigned blocks = (runs + 7) / 8 * 8 * run;
   const auto go = [&](auto d) {
     constexpr int D = decltype(d)::value;
     if (s.row_tile == 64) attend_many<D, 2><<<blocks, 128, 0, st>>>(v, a, l, run);
