@@ -347,45 +347,89 @@ __global__ __launch_bounds__(kThreads) void attend_few(PagedView v, AttendArgs a
         O += *reinterpret_cast<const f32x4*>(&ow[w][row][c]) * f;
       }
       const int r = r0 + 16 * nb + row;
+      if (r >= rows) continue;
       if (live > 1) {
         const size_t rec = ((size_t)unit * a.n_split + split) * kRows + 16 * nb + row;
         *reinterpret_cast<f32x4*>(a.part + rec * D + c) = O;
         if (c == 0) a.stat[rec] = float2{M, L};
-      } else if (r < rows) {
+      } else {
         store_row<T>(a, v, layer, g, hpg, ts.row0, r, c, M, L, O);
       }
     }
   }
 }
 
-// The splits of a row tile joined in split order, D/4 threads per row.
+// The splits of a row joined: D/4 threads for four columns each, times
+// `groups` that take every groups-th split and are joined through LDS.  The
+// order is fixed by the numbers of splits alone.
 template <typename T, int D, int TT>
 __global__ __launch_bounds__(kThreads) void attend_join(PagedView v, AttendArgs a, AttendLists s,
-                                                        int row_tile) {
-  constexpr int kPerRow = D / 4, kRowsHere = kThreads / kPerRow;
-  const int steps = row_tile / kRowsHere;
-  const int unit = blockIdx.x / steps, row = blockIdx.x % steps * kRowsHere + threadIdx.x / kPerRow;
-  const int c = threadIdx.x % kPerRow * 4;
+                                                        int row_tile, int groups) {
+  constexpr int kPerRow = D / 4, kSlots = kThreads / kPerRow;
+  __shared__ __align__(16) float oo[kSlots][D];
+  __shared__ float2 ss[kSlots];
+  const int slot = threadIdx.x / kPerRow, c = threadIdx.x % kPerRow * 4;
+  const int group = slot & (groups - 1), here = kSlots / groups, steps = row_tile / here;
+  const int unit = blockIdx.x / steps, row = blockIdx.x % steps * here + slot / groups;
   const int tile = unit % a.n_tiles, lg = unit / a.n_tiles;
   const int g = lg % v.G, layer = lg / v.G, hpg = v.H / v.G;
   const int b = tile_owner(s.tile0, s.r.n, tile);
   const TokenSpan ts = token_span<TT>(v, a, s, b, tile, row_tile);
   const int live = (ts.nt + ts.per - 1) / ts.per;
   const int r = (tile - s.tile0[b]) * row_tile + row;
-  if (live <= 1 || r >= ts.T * hpg) return;
+  const bool there = live > 1 && r < ts.T * hpg;
   const size_t rec = (size_t)unit * a.n_split * row_tile + row;
   float M = -INFINITY, L = 0.f;
   f32x4 O{0.f, 0.f, 0.f, 0.f};
-  for (int u = 0; u < live; ++u) M = fmaxf(M, a.stat[rec + (size_t)u * row_tile].x);
-#pragma unroll 4
-  for (int u = 0; u < live; ++u) {
-    const size_t at = rec + (size_t)u * row_tile;
-    const float2 st = a.stat[at];
-    const float f = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((st.x - M) * a.scale);
-    L += st.y * f;
-    O += *reinterpret_cast<const f32x4*>(a.part + at * D + c) * f;
+  if (there)
+    for (int u0 = group; u0 < live; u0 += 4 * groups) {
+      float2 st[4];
+      f32x4 part[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int u = u0 + j * groups;
+        st[j] = float2{-INFINITY, 0.f};
+        part[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (u < live) {
+          const size_t at = rec + (size_t)u * row_tile;
+          st[j] = a.stat[at];
+          part[j] = *reinterpret_cast<const f32x4*>(a.part + at * D + c);
+        }
+      }
+      float top = M;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) top = fmaxf(top, st[j].x);
+      const float ref = top == -INFINITY ? 0.f : top;
+      const float old = __builtin_amdgcn_exp2f((M - ref) * a.scale);
+      M = top;
+      L *= old;
+      O *= old;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float f = __builtin_amdgcn_exp2f((st[j].x - ref) * a.scale);
+        L += st[j].y * f;
+        O += part[j] * f;
+      }
+    }
+  if (groups > 1) {
+    *reinterpret_cast<f32x4*>(&oo[slot][c]) = O;
+    if (c == 0) ss[slot] = float2{M, L};
+    __syncthreads();
+    if (group) return;
+    float top = M;
+    for (int j = 1; j < groups; ++j) top = fmaxf(top, ss[slot + j].x);
+    const float ref = top == -INFINITY ? 0.f : top;
+    const float mine = __builtin_amdgcn_exp2f((M - ref) * a.scale);
+    L *= mine;
+    O *= mine;
+    for (int j = 1; j < groups; ++j) {
+      const float f = __builtin_amdgcn_exp2f((ss[slot + j].x - ref) * a.scale);
+      L += ss[slot + j].y * f;
+      O += *reinterpret_cast<const f32x4*>(&oo[slot + j][c]) * f;
+    }
+    M = top;
   }
-  store_row<T>(a, v, layer, g, hpg, ts.row0, r, c, M, L, O);
+  if (there) store_row<T>(a, v, layer, g, hpg, ts.row0, r, c, M, L, O);
 }
 
 template <typename T, int D>
@@ -401,10 +445,13 @@ int launch(const PagedView& v, const AttendArgs& a, const AttendLists& l, const 
     attend_few<T, D, 2><<<blocks, kThreads, 0, st>>>(v, a, l);
   }
   if (s.n_split > 1) {
-    const int steps = s.row_tile / (kThreads / (D / 4));
-    const unsigned joins = (unsigned)(s.units * steps);
-    if (s.many) attend_join<T, D, 64><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile);
-    else attend_join<T, D, kStep><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile);
+    // up to four splits for each thread
+    constexpr int kSlots = kThreads / (D / 4);
+    int groups = 1;
+    while (groups < kSlots && groups * 4 < s.n_split) groups *= 2;
+    const unsigned joins = (unsigned)(s.units * (s.row_tile / (kSlots / groups)));
+    if (s.many) attend_join<T, D, 64><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile, groups);
+    else attend_join<T, D, kStep><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile, groups);
   }
   return (int)hipGetLastError();
 }

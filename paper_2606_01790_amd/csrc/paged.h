@@ -94,9 +94,10 @@ struct AttendCall {
   int window, sinks;      // no mask: window > 0
 };
 
-// The shape of a call over `rows`, and the first tile of each sequence.
+// The shape of a call over `rows` (window 0: none, or a tree), and the first
+// tile of each sequence.
 starkv_status attend_shape(const PagedView& v, const int32_t* rows, int n, int32_t max_len,
-                           AttendShape* s, int32_t* tile0);
+                           int32_t window, int32_t sinks, AttendShape* s, int32_t* tile0);
 int launch_attend(const PagedView& v, const AttendCall& c, void* stream);
 
 }  // namespace starkv

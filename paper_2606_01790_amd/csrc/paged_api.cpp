@@ -112,8 +112,40 @@ starkv_status take_rows(const PagedView& v, const int32_t* slots, const int32_t*
 
 }  // namespace
 
+namespace {
+
+// How many splits a (layer, group, row tile)'s steps are divided into, at
+// most `most`.
+int split_count(const AttendShape& s, int d, int64_t steps, int64_t most) {
+  if (s.units == 0) return 1;
+  if (!s.many) {
+    // bound by HBM: enough blocks to fill the CUs some times over, of at
+    // least four steps (one for each wave), eight where there are many
+    const int64_t min_steps = s.units * ((steps + 3) / 4) <= 1024 ? 4 : 8;
+    const int64_t ns = std::min((steps + min_steps - 1) / min_steps, std::max<int64_t>(1, 2048 / s.units));
+    return (int)std::max<int64_t>(1, std::min(ns, most));
+  }
+  // bound by the matrix units: rounds of the 512 blocks that the card holds,
+  // each as long as a split's steps and the four that a block's start and
+  // end are worth; joining costs two steps and one per 10 MB of partial sums
+  double best = 0;
+  int best_ns = 1;
+  const int64_t top = std::min({steps, most, std::max<int64_t>(1, 4096 / s.units)});
+  for (int64_t ns = 1; ns <= top; ++ns) {
+    double cost = (double)((s.units * ns + 511) / 512) * (double)((steps + ns - 1) / ns + 4);
+    if (ns > 1) cost += 2 + (double)(s.units * ns) * s.row_tile * d * 8 / 10e6;
+    if (ns == 1 || cost < best) {
+      best = cost;
+      best_ns = (int)ns;
+    }
+  }
+  return best_ns;
+}
+
+}  // namespace
+
 starkv_status attend_shape(const PagedView& v, const int32_t* rows, int n, int32_t max_len,
-                           AttendShape* s, int32_t* tile0) {
+                           int32_t window, int32_t sinks, AttendShape* s, int32_t* tile0) {
   if (n < 0 || n > kMaxSeqs) return STARKV_E_PARAM;
   if (n > 0 && !rows) return STARKV_E_NULL;
   if (max_len < 1 || max_len > kMaxTokens) return STARKV_E_PARAM;
@@ -140,18 +172,22 @@ starkv_status attend_shape(const PagedView& v, const int32_t* rows, int n, int32
   }
   if (tile0) tile0[n] = (int32_t)tiles;
   s->units = tiles * v.n_layers * v.G;
+  // Splits for the tokens that one row tile may see.  The workspace is that
+  // of a call without a window, whose splits bound those of one with it.
   const int64_t len = std::min<int64_t>(max_len, v.cap);
-  // splits of at least 256 tokens, two tiles for each of a block's waves,
-  // and no more than fill the CUs some times over
-  int64_t chunk = (len * s->units / 4096 + 127) / 128 * 128;
-  chunk = std::max<int64_t>(chunk, 256);
-  s->chunk = (int)std::min<int64_t>(chunk, kMaxTokens);
-  s->n_split = (int)std::max<int64_t>(1, (len + s->chunk - 1) / s->chunk);
-  if (tiles > INT32_MAX || s->units * s->n_split > INT32_MAX) return STARKV_E_PARAM;
+  const int step = s->many ? 64 : 32;
+  const int most_split = split_count(*s, v.d, (len + step - 1) / step, INT32_MAX);
+  const int64_t row_tokens = (s->row_tile + hpg - 1) / hpg + 1;
+  const int64_t seen = window ? std::min<int64_t>(len, (int64_t)window + sinks + row_tokens + 2 * step)
+                              : len;
+  const int64_t steps = std::max<int64_t>(1, (seen + step - 1) / step);
+  s->n_split = split_count(*s, v.d, steps, most_split);
+  s->chunk = (int)((steps + s->n_split - 1) / s->n_split * step);
+  if (tiles > INT32_MAX || s->units * most_split > INT32_MAX / 16) return STARKV_E_PARAM;
   s->n_tiles = (int)tiles;
   s->stat_off = s->ws_bytes = 0;
-  if (s->n_split > 1) {
-    const size_t rec = (size_t)s->units * s->n_split * s->row_tile;
+  if (most_split > 1) {
+    const size_t rec = (size_t)s->units * most_split * s->row_tile;
     s->stat_off = up256(rec * v.d * sizeof(float));
     s->ws_bytes = s->stat_off + up256(rec * 2 * sizeof(float));
   }
@@ -167,7 +203,8 @@ starkv_status attend(const starkv_paged* cache, const int32_t* slots, int32_t n,
   starkv_status st = check_paged(cache, &v);
   if (st != STARKV_OK) return st;
   if ((st = check_slots(v, slots, n, false)) != STARKV_OK) return st;
-  if ((st = attend_shape(v, rows, n, max_len, &c->s, c->tile0)) != STARKV_OK) return st;
+  if ((st = attend_shape(v, rows, n, max_len, c->words ? 0 : c->window, c->sinks, &c->s,
+                         c->tile0)) != STARKV_OK) return st;
   if (c->words)
     for (int b = 0; b < n; ++b)
       if (rows[b] > 64 * c->words) return STARKV_E_PARAM;
@@ -324,7 +361,7 @@ size_t starkv_attend_workspace_bytes(const starkv_paged* cache, const int32_t* r
   PagedView v;
   AttendShape s;
   if (check_paged(cache, &v) != STARKV_OK ||
-      attend_shape(v, rows, n, max_len, &s, nullptr) != STARKV_OK)
+      attend_shape(v, rows, n, max_len, 0, 0, &s, nullptr) != STARKV_OK)
     return 0;
   return s.ws_bytes;
 }

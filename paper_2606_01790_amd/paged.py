@@ -11,6 +11,7 @@ current) stream.  All compute happens in the library's HIP kernels.
 from __future__ import annotations
 
 import ctypes
+from array import array
 from ctypes import POINTER, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
@@ -143,7 +144,8 @@ def rows_layout(t) -> KVLayout:
 # ------------------------------------------------------------------ marshalling
 
 def _ints(x):
-    return (c_int32 * len(x))(*x)
+    """A host list as int32; _run passes its address."""
+    return array("i", x)
 
 
 def _ptr(t):
@@ -151,13 +153,18 @@ def _ptr(t):
 
 
 def _run(name, cache, stream, *args):
-    fn = getattr(lib(), name)
+    fn = getattr(_lib or lib(), name)
     index = cache.device.index
-    if torch.cuda.current_device() == index:
-        code = fn(cache.ref, *args, sk._stream(stream))
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(index)
+    else:
+        stream = getattr(stream, "cuda_stream", stream)
+    at = [x.buffer_info()[0] if type(x) is array else x for x in args]   # args keeps the arrays
+    if torch._C._cuda_getDevice() == index:
+        code = fn(cache.ref, *at, stream)
     else:
         with torch.cuda.device(index):
-            code = fn(cache.ref, *args, sk._stream(stream))
+            code = fn(cache.ref, *at, stream)
     if code != 0:
         raise StarKVError(name, code)
 
@@ -257,7 +264,9 @@ def pages_compact(cache: Cache, slots, idx, status, ws, tail: int = 0, span=None
 # ------------------------------------------------------------------ attention
 
 def attend_workspace_bytes(cache: Cache, rows, max_len: int) -> int:
-    return int(lib().starkv_attend_workspace_bytes(cache.ref, _ints(rows), len(rows), max_len))
+    rows = _ints(rows)
+    return int(lib().starkv_attend_workspace_bytes(cache.ref, rows.buffer_info()[0], len(rows),
+                                                   max_len))
 
 
 def _attend_args(cache, slots, rows, q, out, lse, ws):
