@@ -17,6 +17,8 @@ struct AttendArgs {
   const uint64_t* mask;
   int words, window, sinks;
   int n_split, chunk, n_tiles, n_rows;
+  int most_steps;         // the most steps of a row tile
+  int* steps;             // the steps of a split that the device chose, or NULL
   float scale;            // log2(e) / sqrt(d)
 };
 
@@ -56,7 +58,8 @@ struct TokenSpan {
 
 template <int TT>
 __device__ inline TokenSpan token_span(const PagedView& v, const AttendArgs& a,
-                                       const AttendLists& s, int b, int tile, int row_tile) {
+                                       const AttendLists& s, int b, int tile, int row_tile,
+                                       int chosen = 0) {
   TokenSpan t;
   const int hpg = v.H / v.G;
   t.n = min(max(const_ints(v.len)[s.r.slot[b]], 0), v.cap);
@@ -76,8 +79,49 @@ __device__ inline TokenSpan token_span(const PagedView& v, const AttendArgs& a,
   t.nt = t.ns + (t.hi - t.lo + TT - 1) / TT;
   // a split takes chunk tokens, or more where the lengths exceed the bound
   // that the number of splits was made for
-  t.per = max((a.chunk + TT - 1) / TT, (t.nt + a.n_split - 1) / a.n_split);
+  t.per = max(chosen ? chosen : (a.chunk + TT - 1) / TT, (t.nt + a.n_split - 1) / a.n_split);
   return t;
+}
+
+// The steps of a split, for sequences whose lengths only the device knows:
+// the least with which the blocks of all splits fit the `slots` that the card
+// holds at a time, or as many times as leave about 96 steps to a block.  The
+// lanes of a wave take a sequence each.
+template <int TT>
+__device__ inline int balanced_steps(const PagedView& v, const AttendArgs& a, const AttendLists& s,
+                                     int slots) {
+  constexpr int kPer = kMaxSeqs / 64;
+  const int lane = threadIdx.x & 63;
+  int tiles[kPer], steps[kPer], work = 0;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int b = lane + 64 * j;
+    tiles[j] = steps[j] = 0;
+    if (b < s.r.n) {
+      tiles[j] = s.tile0[b + 1] - s.tile0[b];
+      const int n = min(max(v.len[s.r.slot[b]], 0), v.cap);
+      steps[j] = min((n + TT - 1) / TT, a.most_steps);
+    }
+    work += tiles[j] * steps[j];
+  }
+  const auto all = [](int x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+    return x;
+  };
+  work = all(work);
+  const int lgs = v.n_layers * v.G;
+  const float rounds = fmaxf(1.f, rintf((float)work * (float)lgs / (float)(slots * 96)));
+  const int target = max(1, (int)((float)slots * rounds / (float)lgs));   // blocks of a (layer, group)
+  int per = max(4, (work + target - 1) / target);
+  for (int i = 0; i < 16; ++i) {
+    int blocks = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) blocks += tiles[j] * ((steps[j] + per - 1) / per);
+    if (all(blocks) <= target) break;
+    per += max(1, per >> 4);
+  }
+  return __builtin_amdgcn_readfirstlane(per);
 }
 
 // Token of step u's first.

@@ -20,6 +20,8 @@
 //                 columns, of each of its eight tokens and swaps them into eight
 //                 fragments with 32 v_perm, so V needs no LDS either.
 // float32 caches run the same scheme on the 16x16x4 MFMA, four per 16 bytes.
+#include <algorithm>
+
 #include "attend.h"
 
 namespace starkv {
@@ -361,75 +363,81 @@ __global__ __launch_bounds__(kThreads) void attend_few(PagedView v, AttendArgs a
 
 // The splits of a row joined: D/4 threads for four columns each, times
 // `groups` that take every groups-th split and are joined through LDS.  The
-// order is fixed by the numbers of splits alone.
+// order is fixed by the numbers of splits alone.  `parts` blocks share a row
+// tile, each with every parts-th handful of its rows.
 template <typename T, int D, int TT>
 __global__ __launch_bounds__(kThreads) void attend_join(PagedView v, AttendArgs a, AttendLists s,
-                                                        int row_tile, int groups) {
+                                                        int row_tile, int groups, int parts) {
   constexpr int kPerRow = D / 4, kSlots = kThreads / kPerRow;
   __shared__ __align__(16) float oo[kSlots][D];
   __shared__ float2 ss[kSlots];
   const int slot = threadIdx.x / kPerRow, c = threadIdx.x % kPerRow * 4;
-  const int group = slot & (groups - 1), here = kSlots / groups, steps = row_tile / here;
-  const int unit = blockIdx.x / steps, row = blockIdx.x % steps * here + slot / groups;
+  const int group = slot & (groups - 1), here = kSlots / groups;
+  const int unit = blockIdx.x / parts, part = blockIdx.x % parts;
   const int tile = unit % a.n_tiles, lg = unit / a.n_tiles;
   const int g = lg % v.G, layer = lg / v.G, hpg = v.H / v.G;
   const int b = tile_owner(s.tile0, s.r.n, tile);
-  const TokenSpan ts = token_span<TT>(v, a, s, b, tile, row_tile);
+  const TokenSpan ts = token_span<TT>(v, a, s, b, tile, row_tile, a.steps ? *a.steps : 0);
   const int live = (ts.nt + ts.per - 1) / ts.per;
-  const int r = (tile - s.tile0[b]) * row_tile + row;
-  const bool there = live > 1 && r < ts.T * hpg;
-  const size_t rec = (size_t)unit * a.n_split * row_tile + row;
-  float M = -INFINITY, L = 0.f;
-  f32x4 O{0.f, 0.f, 0.f, 0.f};
-  if (there)
-    for (int u0 = group; u0 < live; u0 += 4 * groups) {
-      float2 st[4];
-      f32x4 part[4];
+  const int r0 = (tile - s.tile0[b]) * row_tile, rows = min(ts.T * hpg - r0, row_tile);
+  if (live <= 1) return;
+  for (int first = part * here; first < rows; first += parts * here) {
+    const int row = first + slot / groups;
+    const size_t rec = (size_t)unit * a.n_split * row_tile + row;
+    float M = -INFINITY, L = 0.f;
+    f32x4 O{0.f, 0.f, 0.f, 0.f};
+    if (row < rows)
+      for (int u0 = group; u0 < live; u0 += 4 * groups) {
+        float2 st[4];
+        f32x4 piece[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int u = u0 + j * groups;
-        st[j] = float2{-INFINITY, 0.f};
-        part[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (u < live) {
-          const size_t at = rec + (size_t)u * row_tile;
-          st[j] = a.stat[at];
-          part[j] = *reinterpret_cast<const f32x4*>(a.part + at * D + c);
+        for (int j = 0; j < 4; ++j) {
+          const int u = u0 + j * groups;
+          st[j] = float2{-INFINITY, 0.f};
+          piece[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if (u < live) {
+            const size_t at = rec + (size_t)u * row_tile;
+            st[j] = a.stat[at];
+            piece[j] = *reinterpret_cast<const f32x4*>(a.part + at * D + c);
+          }
+        }
+        float top = M;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, st[j].x);
+        const float ref = top == -INFINITY ? 0.f : top;
+        const float old = __builtin_amdgcn_exp2f((M - ref) * a.scale);
+        M = top;
+        L *= old;
+        O *= old;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float f = __builtin_amdgcn_exp2f((st[j].x - ref) * a.scale);
+          L += st[j].y * f;
+          O += piece[j] * f;
         }
       }
-      float top = M;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) top = fmaxf(top, st[j].x);
-      const float ref = top == -INFINITY ? 0.f : top;
-      const float old = __builtin_amdgcn_exp2f((M - ref) * a.scale);
-      M = top;
-      L *= old;
-      O *= old;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float f = __builtin_amdgcn_exp2f((st[j].x - ref) * a.scale);
-        L += st[j].y * f;
-        O += part[j] * f;
+    if (groups > 1) {
+      __syncthreads();   // the rows before are read
+      *reinterpret_cast<f32x4*>(&oo[slot][c]) = O;
+      if (c == 0) ss[slot] = float2{M, L};
+      __syncthreads();
+      if (group == 0) {
+        float top = M;
+        for (int j = 1; j < groups; ++j) top = fmaxf(top, ss[slot + j].x);
+        const float ref = top == -INFINITY ? 0.f : top;
+        const float mine = __builtin_amdgcn_exp2f((M - ref) * a.scale);
+        L *= mine;
+        O *= mine;
+        for (int j = 1; j < groups; ++j) {
+          const float f = __builtin_amdgcn_exp2f((ss[slot + j].x - ref) * a.scale);
+          L += ss[slot + j].y * f;
+          O += *reinterpret_cast<const f32x4*>(&oo[slot + j][c]) * f;
+        }
+        M = top;
       }
     }
-  if (groups > 1) {
-    *reinterpret_cast<f32x4*>(&oo[slot][c]) = O;
-    if (c == 0) ss[slot] = float2{M, L};
-    __syncthreads();
-    if (group) return;
-    float top = M;
-    for (int j = 1; j < groups; ++j) top = fmaxf(top, ss[slot + j].x);
-    const float ref = top == -INFINITY ? 0.f : top;
-    const float mine = __builtin_amdgcn_exp2f((M - ref) * a.scale);
-    L *= mine;
-    O *= mine;
-    for (int j = 1; j < groups; ++j) {
-      const float f = __builtin_amdgcn_exp2f((ss[slot + j].x - ref) * a.scale);
-      L += ss[slot + j].y * f;
-      O += *reinterpret_cast<const f32x4*>(&oo[slot + j][c]) * f;
-    }
-    M = top;
+    if (group == 0 && row < rows) store_row<T>(a, v, layer, g, hpg, ts.row0, r0 + row, c, M, L, O);
   }
-  if (there) store_row<T>(a, v, layer, g, hpg, ts.row0, r, c, M, L, O);
 }
 
 template <typename T, int D>
@@ -441,7 +449,7 @@ int launch(const PagedView& v, const AttendArgs& a, const AttendLists& l, const 
     if (err) return err;
   } else if (s.row_tile == 16) {
     attend_few<T, D, 1><<<blocks, kThreads, 0, st>>>(v, a, l);
-  } else {
+  } else if constexpr (sizeof(T) == 2) {
     attend_few<T, D, 2><<<blocks, kThreads, 0, st>>>(v, a, l);
   }
   if (s.n_split > 1) {
@@ -449,9 +457,11 @@ int launch(const PagedView& v, const AttendArgs& a, const AttendLists& l, const 
     constexpr int kSlots = kThreads / (D / 4);
     int groups = 1;
     while (groups < kSlots && groups * 4 < s.n_split) groups *= 2;
-    const unsigned joins = (unsigned)(s.units * (s.row_tile / (kSlots / groups)));
-    if (s.many) attend_join<T, D, 64><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile, groups);
-    else attend_join<T, D, kStep><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile, groups);
+    const int handfuls = s.row_tile / (kSlots / groups);
+    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(handfuls, 2048 / s.units));
+    const unsigned joins = (unsigned)(s.units * parts);
+    if (s.many) attend_join<T, D, 64><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile, groups, parts);
+    else attend_join<T, D, kStep><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile, groups, parts);
   }
   return (int)hipGetLastError();
 }
@@ -473,6 +483,8 @@ int launch_attend(const PagedView& v, const AttendCall& c, void* stream) {
   a.n_split = c.s.n_split;
   a.chunk = c.s.chunk;
   a.n_tiles = c.s.n_tiles;
+  a.most_steps = c.s.steps;
+  a.steps = c.s.balance ? reinterpret_cast<int*>(static_cast<char*>(c.ws) + c.s.steps_off) : nullptr;
   a.n_rows = c.s.n_rows;
   a.scale = 1.4426950408889634f / sqrtf((float)v.d);
   AttendLists l;

@@ -17,14 +17,15 @@
 // then the weights, up to 2^8, lose nothing, and the output need not be
 // rescaled.
 #include <algorithm>
-#include <type_traits>
 
 #include "attend.h"
 
 namespace starkv {
 namespace {
 
+constexpr int kWaves = 4;
 constexpr int kStep = 64;
+constexpr int kBlocks = 512;             // that the card holds at a time
 constexpr int kGroups = kStep / 16;      // 16-token groups of a step: one page each
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -87,10 +88,9 @@ __device__ inline unsigned xcd_item(unsigned block, unsigned run) {
   return (i / run * 8 + xcd) * run + i % run;
 }
 
-template <int D, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(PagedView v, AttendArgs a,
-                                                             AttendLists s, unsigned run) {
-  constexpr int kMine = kGroups / WAVES;   // 16-token groups of a step that a wave stages
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, 2) void attend_many(PagedView v, AttendArgs a,
+                                                              AttendLists s, unsigned run) {
   constexpr int NF = D / 16;               // k-steps of S
   constexpr int ND = D / 32;               // 32-column tiles of the output
   constexpr int kRow = D * 2;              // bytes of a row
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
 
   const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  constexpr int row_tile = WAVES * 32;
+  constexpr int row_tile = kWaves * 32;
   // `run` tiles of one split of a (layer, group) follow each other: they read
   // the same K and V.  Later tiles, which may see more, come first, those of
   // all (layer, group)s together
@@ -108,10 +108,12 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
   const unsigned lgs = v.n_layers * v.G, runs = (a.n_tiles + run - 1) / run, at_run = item / run;
   const int lg = at_run % lgs, split = at_run / lgs / runs;
   const int tile = a.n_tiles - 1 - (int)(at_run / lgs % runs * run + item % run);
+  const int chosen = a.steps ? balanced_steps<kStep>(v, a, s, kBlocks) : 0;
+  if (a.steps && blockIdx.x == 0 && threadIdx.x == 0) *a.steps = chosen;   // for the join
   if (split >= a.n_split || tile < 0) return;
   const int g = lg % v.G, layer = lg / v.G;
   const int b = tile_owner(s.tile0, s.r.n, tile);
-  const TokenSpan ts = token_span<kStep>(v, a, s, b, tile, row_tile);
+  const TokenSpan ts = token_span<kStep>(v, a, s, b, tile, row_tile, chosen);
   const int live = (ts.nt + ts.per - 1) / ts.per;
   if (split >= max(live, 1)) return;
   const int hpg = v.H / v.G;
@@ -145,7 +147,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
   const int64_t base = (int64_t)layer * v.ls + (int64_t)g * v.gs;
   const int u0 = split * ts.per, u1 = min(u0 + ts.per, ts.nt);
   // The pages of a step's four groups, and from them which have none (bit by
-  // bit) and where the groups that this wave stages lie in the pool
+  // bit) and where the one that this wave stages lies in the pool
   using Pages = i32x4;
   const auto pages_at = [&](int u) {
     const int t = step_token<kStep>(ts, min(u, ts.nt - 1));
@@ -160,23 +162,18 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
     return ((unsigned)p[0] >= n ? 1u : 0u) | ((unsigned)p[1] >= n ? 2u : 0u) |
            ((unsigned)p[2] >= n ? 4u : 0u) | ((unsigned)p[3] >= n ? 8u : 0u);
   };
-  const auto where = [&](int u, const Pages& p, int i) {
-    const int grp = wave * kMine + i;
-    unsigned page = grp < 2 ? (grp < 1 ? p[0] : p[1]) : (grp < 3 ? p[2] : p[3]);
+  const auto where = [&](int u, const Pages& p) {
+    unsigned page = wave < 2 ? (wave < 1 ? p[0] : p[1]) : (wave < 3 ? p[2] : p[3]);
     if (page >= (unsigned)v.n_pages) page = 0;      // masked in the step
-    const unsigned row = (unsigned)(step_token<kStep>(ts, min(u, ts.nt - 1)) + 16 * grp) &
+    const unsigned row = (unsigned)(step_token<kStep>(ts, min(u, ts.nt - 1)) + 16 * wave) &
                          (unsigned)(v.P - 1);
     return (uint64_t)base + page * (uint64_t)v.ps + row * (uint64_t)v.ts;
   };
-  const auto load_k = [&](const uint64_t (&at)[kMine], char* to) {
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-      stage<D>(v.k + at[i], v.ts, row_off, kpiece, kturn, to + (wave * kMine + i) * 16 * kRow);
+  const auto load_k = [&](uint64_t at, char* to) {
+    stage<D>(v.k + at, v.ts, row_off, kpiece, kturn, to + wave * 16 * kRow);
   };
-  const auto load_v = [&](const uint64_t (&at)[kMine], char* to) {
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-      stage<D>(v.v + at[i], v.ts, row_off, vpiece, vturn, to + (wave * kMine + i) * 16 * kRow);
+  const auto load_v = [&](uint64_t at, char* to) {
+    stage<D>(v.v + at, v.ts, row_off, vpiece, vturn, to + wave * 16 * kRow);
   };
   const auto landed = [&]() {
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
@@ -226,7 +223,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
   // 1 fills vn.
   // The addresses of the next rows to stage are worked out beside the products
   // with V, the part of a step that is poorest in other work.
-  uint64_t at1[kMine], at2[kMine];           // of steps u + 1 and u + 2
+  uint64_t at1 = 0, at2 = 0;                 // of steps u + 1 and u + 2
   unsigned hole0 = 0, hole1 = 0, hole2 = 0;  // groups without a page, of u and the next two
   const auto step = [&](int u, const char* kn, char* kf, char* vs, char* vn) {
     // the loads are complete, and every wave is done with what they replace
@@ -246,7 +243,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
       held &= (uint64_t)low_bits(ts.n - t0) | (uint64_t)low_bits(ts.n - t0 - 32) << 32;
       // some rows do not see all of it.  What no page holds counts as zero;
       // infinities and NaN of V need the way below
-      for (int i = here(threadIdx.x); i < kStep * NP; i += 64 * WAVES) {
+      for (int i = here(threadIdx.x); i < kStep * NP; i += 64 * kWaves) {
         const int token = i / NP;
         u32x4* at = reinterpret_cast<u32x4*>(vs + i * 16);
         if (!(held >> token & 1)) {
@@ -356,7 +353,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
         }
       }
       __syncthreads();
-      for (int i = here(threadIdx.x); i < kStep * NP; i += 64 * WAVES) {
+      for (int i = here(threadIdx.x); i < kStep * NP; i += 64 * kWaves) {
         u32x4 w = *reinterpret_cast<u32x4*>(vs + i * 16);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -373,15 +370,10 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
     }
     hole0 = hole1;
     hole1 = hole2;
-    uint64_t at3[kMine];
     const auto look_ahead = [&]() {
       hole2 = holes_of(ahead);
-#pragma unroll
-      for (int i = 0; i < kMine; ++i) {
-        at3[i] = where(u + 3, ahead, i);
-        at1[i] = at2[i];
-        at2[i] = at3[i];
-      }
+      at1 = at2;
+      at2 = where(u + 3, ahead);
     };
     if (idle) {
       look_ahead();
@@ -416,13 +408,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 2 ? 1 : 2) void attend_many(Pa
     hole0 = holes_of(p0);
     hole1 = holes_of(p1);
     hole2 = holes_of(p2);
-    uint64_t at0[kMine];
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      at0[i] = where(u0, p0, i);
-      at1[i] = where(u0 + 1, p1, i);
-      at2[i] = where(u0 + 2, p2, i);
-    }
+    const uint64_t at0 = where(u0, p0);
+    at1 = where(u0 + 1, p1);
+    at2 = where(u0 + 2, p2);
     load_k(at0, k0);
     load_v(at0, v0);
     if (u0 + 1 < u1) load_k(at1, k1);
@@ -474,13 +462,8 @@ int launch_attend_many(const PagedView& v, const AttendArgs& a, const AttendList
   const unsigned run = (unsigned)std::min(s.n_tiles, 4);
   const unsigned runs = (unsigned)((s.n_tiles + run - 1) / run) * v.n_layers * v.G * s.n_split;
   const unsigned blocks = (runs + 7) / 8 * 8 * run;
-  const auto go = [&](auto d) {
-    constexpr int D = decltype(d)::value;
-    if (s.row_tile == 64) attend_many<D, 2><<<blocks, 128, 0, st>>>(v, a, l, run);
-    else attend_many<D, 4><<<blocks, 256, 0, st>>>(v, a, l, run);
-  };
-  if (v.d == 128) go(std::integral_constant<int, 128>{});
-  else go(std::integral_constant<int, 64>{});
+  if (v.d == 128) attend_many<128><<<blocks, 64 * kWaves, 0, st>>>(v, a, l, run);
+  else attend_many<64><<<blocks, 64 * kWaves, 0, st>>>(v, a, l, run);
   return (int)hipGetLastError();
 }
 

@@ -76,8 +76,11 @@ struct AttendShape {
   int n_tiles;      // row tiles of one (layer, group), over all sequences
   int n_split;      // splits of the tokens
   int chunk;        // tokens that a split takes at least
+  int steps;        // the most steps that a row tile walks
+  bool balance;     // the device divides the steps (several sequences)
   int64_t units;    // n_layers * G * n_tiles
   size_t stat_off;  // bytes: the partial statistics behind the partial outputs
+  size_t steps_off; // the device's steps of a split
   size_t ws_bytes;
 };
 

@@ -115,8 +115,8 @@ starkv_status take_rows(const PagedView& v, const int32_t* slots, const int32_t*
 namespace {
 
 // How many splits a (layer, group, row tile)'s steps are divided into, at
-// most `most`.
-int split_count(const AttendShape& s, int d, int64_t steps, int64_t most) {
+// most `most`, in a call of n sequences.
+int split_count(const AttendShape& s, int n, int d, int64_t steps, int64_t most) {
   if (s.units == 0) return 1;
   if (!s.many) {
     // bound by HBM: enough blocks to fill the CUs some times over, of at
@@ -125,13 +125,18 @@ int split_count(const AttendShape& s, int d, int64_t steps, int64_t most) {
     const int64_t ns = std::min((steps + min_steps - 1) / min_steps, std::max<int64_t>(1, 2048 / s.units));
     return (int)std::max<int64_t>(1, std::min(ns, most));
   }
+  const int64_t top = std::min(steps, most);
+  if (n > 1) {
+    // lengths that only the device knows: it divides the steps itself, into
+    // at most this many splits
+    return (int)std::min(top, std::max<int64_t>(1, 2048 / s.units));
+  }
   // bound by the matrix units: rounds of the 512 blocks that the card holds,
   // each as long as a split's steps and the four that a block's start and
   // end are worth; joining costs two steps and one per 10 MB of partial sums
   double best = 0;
   int best_ns = 1;
-  const int64_t top = std::min({steps, most, std::max<int64_t>(1, 4096 / s.units)});
-  for (int64_t ns = 1; ns <= top; ++ns) {
+  for (int64_t ns = 1; ns <= std::min<int64_t>(top, std::max<int64_t>(1, 4096 / s.units)); ++ns) {
     double cost = (double)((s.units * ns + 511) / 512) * (double)((steps + ns - 1) / ns + 4);
     if (ns > 1) cost += 2 + (double)(s.units * ns) * s.row_tile * d * 8 / 10e6;
     if (ns == 1 || cost < best) {
@@ -160,11 +165,7 @@ starkv_status attend_shape(const PagedView& v, const int32_t* rows, int n, int32
   s->n_rows = (int)tot;
   const int64_t R = most * hpg;
   s->many = v.esz == 2 && R > 32;
-  if (s->many) {
-    s->row_tile = R <= 64 ? 64 : 128;
-  } else {
-    s->row_tile = R <= 16 ? 16 : 32;
-  }
+  s->row_tile = s->many ? 128 : v.esz == 2 && R > 16 ? 32 : 16;
   int64_t tiles = 0;
   for (int b = 0; b < n; ++b) {
     if (tile0) tile0[b] = (int32_t)tiles;
@@ -176,20 +177,23 @@ starkv_status attend_shape(const PagedView& v, const int32_t* rows, int n, int32
   // of a call without a window, whose splits bound those of one with it.
   const int64_t len = std::min<int64_t>(max_len, v.cap);
   const int step = s->many ? 64 : 32;
-  const int most_split = split_count(*s, v.d, (len + step - 1) / step, INT32_MAX);
+  const int most_split = split_count(*s, n, v.d, (len + step - 1) / step, INT32_MAX);
   const int64_t row_tokens = (s->row_tile + hpg - 1) / hpg + 1;
   const int64_t seen = window ? std::min<int64_t>(len, (int64_t)window + sinks + row_tokens + 2 * step)
                               : len;
   const int64_t steps = std::max<int64_t>(1, (seen + step - 1) / step);
-  s->n_split = split_count(*s, v.d, steps, most_split);
+  s->n_split = split_count(*s, n, v.d, steps, most_split);
   s->chunk = (int)((steps + s->n_split - 1) / s->n_split * step);
   if (tiles > INT32_MAX || s->units * most_split > INT32_MAX / 16) return STARKV_E_PARAM;
   s->n_tiles = (int)tiles;
-  s->stat_off = s->ws_bytes = 0;
+  s->stat_off = s->steps_off = s->ws_bytes = 0;
+  s->steps = (int)steps;
+  s->balance = s->many && n > 1 && s->n_split > 1;
   if (most_split > 1) {
     const size_t rec = (size_t)s->units * most_split * s->row_tile;
     s->stat_off = up256(rec * v.d * sizeof(float));
-    s->ws_bytes = s->stat_off + up256(rec * 2 * sizeof(float));
+    s->steps_off = s->stat_off + up256(rec * 2 * sizeof(float));
+    s->ws_bytes = s->steps_off + 256;
   }
   return STARKV_OK;
 }
