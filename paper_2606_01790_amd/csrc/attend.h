@@ -46,6 +46,15 @@ __device__ inline int tile_owner(const int32_t* first, int n, int k) {
   return __builtin_amdgcn_readfirstlane(count) - 1;
 }
 
+// Blocks are dealt to the 8 XCDs round-robin by number.  Work items that
+// follow each other share K and V: each XCD takes `run` of them in turn, so
+// that its L2 holds what they read, and all XCDs move through the items
+// together, whose costs differ from end to end.
+__device__ inline unsigned xcd_item(unsigned block, unsigned run) {
+  const unsigned xcd = block & 7, i = block >> 3;
+  return (i / run * 8 + xcd) * run + i % run;
+}
+
 // The cached tokens of one row tile.  They are walked in steps of TT tokens:
 // first the sinks' [0, ns*TT), then the window's from lo on, both from
 // multiples of TT, so that no step is in both.

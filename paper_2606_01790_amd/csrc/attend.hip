@@ -113,7 +113,8 @@ __device__ inline void zero_not_finite(R& r) {
 }
 
 template <typename T, int D, int NB>
-__global__ __launch_bounds__(kThreads) void attend_few(PagedView v, AttendArgs a, AttendLists s) {
+__global__ __launch_bounds__(kThreads) void attend_few(PagedView v, AttendArgs a, AttendLists s,
+                                                       unsigned run) {
   using F = Frag<T>;
   using frag = typename F::type;
   using VR = VRow<T, D>;
@@ -128,9 +129,14 @@ __global__ __launch_bounds__(kThreads) void attend_few(PagedView v, AttendArgs a
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, quad = lane >> 4;
-  const int split = blockIdx.x % a.n_split;
-  const int unit = blockIdx.x / a.n_split;
-  const int tile = unit % a.n_tiles, lg = unit / a.n_tiles;
+  // `run` tiles of one split of a (layer, group) follow each other: they read
+  // the same K and V where they are of one sequence
+  const unsigned item = xcd_item(blockIdx.x, run);
+  const unsigned runs = (a.n_tiles + run - 1) / run, at_run = item / run;
+  const int split = at_run % a.n_split, lg = at_run / a.n_split / runs;
+  const int tile = at_run / a.n_split % runs * run + item % run;
+  if (lg >= v.n_layers * v.G || tile >= a.n_tiles) return;
+  const int unit = lg * a.n_tiles + tile;
   const int g = lg % v.G, layer = lg / v.G;
   const int b = tile_owner(s.tile0, s.r.n, tile);
   const TokenSpan ts = token_span<kStep>(v, a, s, b, tile, kRows);
@@ -443,14 +449,16 @@ __global__ __launch_bounds__(kThreads) void attend_join(PagedView v, AttendArgs 
 template <typename T, int D>
 int launch(const PagedView& v, const AttendArgs& a, const AttendLists& l, const AttendShape& s,
            hipStream_t st) {
-  const unsigned blocks = (unsigned)(s.units * s.n_split);
+  const unsigned run = (unsigned)std::min(s.n_tiles, 4);
+  const unsigned runs = (s.n_tiles + run - 1) / run * v.n_layers * v.G * s.n_split;
+  const unsigned blocks = (runs + 7) / 8 * 8 * run;
   if (s.many) {
     const int err = launch_attend_many(v, a, l, s, st);
     if (err) return err;
   } else if (s.row_tile == 16) {
-    attend_few<T, D, 1><<<blocks, kThreads, 0, st>>>(v, a, l);
+    attend_few<T, D, 1><<<blocks, kThreads, 0, st>>>(v, a, l, run);
   } else if constexpr (sizeof(T) == 2) {
-    attend_few<T, D, 2><<<blocks, kThreads, 0, st>>>(v, a, l);
+    attend_few<T, D, 2><<<blocks, kThreads, 0, st>>>(v, a, l, run);
   }
   if (s.n_split > 1) {
     // up to four splits for each thread

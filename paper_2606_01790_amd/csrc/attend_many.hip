@@ -79,15 +79,6 @@ __device__ inline void stage(const char* from, int64_t ts, uint32_t row, uint32_
         (__attribute__((address_space(3))) void*)(to + j * 1024), 16, 0, 0);
 }
 
-// Blocks are dealt to the 8 XCDs round-robin by number.  Work items that
-// follow each other share K and V: each XCD takes `run` of them in turn, so
-// that its L2 holds what they read, and all XCDs move through the items
-// together, whose costs differ from end to end.
-__device__ inline unsigned xcd_item(unsigned block, unsigned run) {
-  const unsigned xcd = block & 7, i = block >> 3;
-  return (i / run * 8 + xcd) * run + i % run;
-}
-
 template <int D>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_many(PagedView v, AttendArgs a,
                                                               AttendLists s, unsigned run) {

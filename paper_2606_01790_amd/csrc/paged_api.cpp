@@ -122,14 +122,14 @@ int split_count(const AttendShape& s, int n, int d, int64_t steps, int64_t most)
     // bound by HBM: enough blocks to fill the CUs some times over, of at
     // least four steps (one for each wave), eight where there are many
     const int64_t min_steps = s.units * ((steps + 3) / 4) <= 1024 ? 4 : 8;
-    const int64_t ns = std::min((steps + min_steps - 1) / min_steps, std::max<int64_t>(1, 2048 / s.units));
+    const int64_t ns = std::min((steps + min_steps - 1) / min_steps, std::max<int64_t>(1, 1024 / s.units));
     return (int)std::max<int64_t>(1, std::min(ns, most));
   }
   const int64_t top = std::min(steps, most);
   if (n > 1) {
     // lengths that only the device knows: it divides the steps itself, into
     // at most this many splits
-    return (int)std::min(top, std::max<int64_t>(1, 2048 / s.units));
+    return (int)std::min(top, std::max<int64_t>(1, 1024 / s.units));
   }
   // bound by the matrix units: rounds of the 512 blocks that the card holds,
   // each as long as a split's steps and the four that a block's start and

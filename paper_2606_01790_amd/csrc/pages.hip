@@ -32,6 +32,31 @@ __device__ inline int32_t* table_row(const PagedView& v, int slot) {
   return v.table + (size_t)slot * v.max_pages;
 }
 
+// The lists of a call, by value.  A launch pays for the bytes of its
+// arguments, so short lists travel in short structs (one slot freed: 5.2 us
+// of the host's time with the long struct, 4.3 with the short one).
+constexpr int kShort = 16;
+template <int N>
+struct Seqs {
+  int32_t n;
+  int32_t slot[N], num[N];
+  explicit Seqs(const SeqList& s) : n(s.n) {
+    for (int i = 0; i < n; ++i) {
+      slot[i] = s.slot[i];
+      num[i] = s.num[i];
+    }
+  }
+};
+template <int N>
+struct Rows {
+  int32_t n;
+  int32_t slot[N], row0[N + 1];
+  explicit Rows(const RowList& r) : n(r.n) {
+    for (int i = 0; i < n; ++i) slot[i] = r.slot[i];
+    for (int i = 0; i <= n; ++i) row0[i] = r.row0[i];
+  }
+};
+
 // The sequence (or tile, or row range) that item k belongs to: the last b
 // with first[b] <= k.
 __device__ inline int owner_of(const int32_t* first, int n, int k) {
@@ -78,7 +103,8 @@ __global__ __launch_bounds__(256) void init_kernel(PagedView v) {
 
 // Pages for the new tokens.  info[b]: the page to copy from (or -1), to, and
 // the rows to copy.
-__global__ __launch_bounds__(kPlanThreads) void grow_plan(PagedView v, SeqList s, int32_t* fresh,
+template <int N>
+__global__ __launch_bounds__(kPlanThreads) void grow_plan(PagedView v, Seqs<N> s, int32_t* fresh,
                                                           i32x4* info, int32_t* status) {
   __shared__ int pre[kMaxSeqs], first[kMaxSeqs], ok[kMaxSeqs], sh[kPlanThreads / 64];
   const int b = threadIdx.x;
@@ -153,8 +179,8 @@ struct WriteArgs {
 
 // One 16-byte vector of K and V per thread.  The page of a token must belong
 // to its sequence alone: a shared one is left as it is.
-template <int VPR>
-__global__ __launch_bounds__(256) void write_kernel(PagedView v, RowList r, WriteArgs a) {
+template <int VPR, int N>
+__global__ __launch_bounds__(256) void write_kernel(PagedView v, Rows<N> r, WriteArgs a) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int part = (int)(i % VPR);
   const int64_t rg = i / VPR;
@@ -174,7 +200,8 @@ __global__ __launch_bounds__(256) void write_kernel(PagedView v, RowList r, Writ
 
 // Sequence s.slot[b] becomes a fork of s.num[b], one pair per block.  No
 // slot is read and written by the same call.
-__global__ __launch_bounds__(256) void fork_kernel(PagedView v, SeqList s) {
+template <int N>
+__global__ __launch_bounds__(256) void fork_kernel(PagedView v, Seqs<N> s) {
   const int b = blockIdx.x, dst = s.slot[b], src = s.num[b];
   const int had = pages_of(v, seq_len(v, dst)), has = pages_of(v, seq_len(v, src));
   int32_t* to = table_row(v, dst);
@@ -190,7 +217,8 @@ __global__ __launch_bounds__(256) void fork_kernel(PagedView v, SeqList s) {
   if (threadIdx.x == 0) v.len[dst] = seq_len(v, src);
 }
 
-__global__ __launch_bounds__(256) void free_kernel(PagedView v, SeqList s, int keep_first,
+template <int N>
+__global__ __launch_bounds__(256) void free_kernel(PagedView v, Seqs<N> s, int keep_first,
                                                    int keep_last) {
   const int slot = s.slot[blockIdx.x], len0 = seq_len(v, slot);
   // dropped tokens: [lo, hi)
@@ -209,7 +237,8 @@ __global__ __launch_bounds__(256) void free_kernel(PagedView v, SeqList s, int k
 // Fresh pages for the kept tokens; the table rows as they were into old[].
 // info[b]: length, a, count (or -1: the sequence stays) and the first fresh
 // page's column.
-__global__ __launch_bounds__(kPlanThreads) void compact_plan(PagedView v, SeqList s, bool whole,
+template <int N>
+__global__ __launch_bounds__(kPlanThreads) void compact_plan(PagedView v, Seqs<N> s, bool whole,
                                                              int B, const int32_t* counts,
                                                              int tail, int32_t* fresh, i32x4* info,
                                                              int32_t* old, int32_t* status) {
@@ -279,8 +308,8 @@ struct MoveArgs {
 
 // The kept rows into the fresh pages, kPer vectors of K and V per thread
 // with their loads in flight together.
-template <int VPR>
-__global__ __launch_bounds__(256) void compact_move(PagedView v, SeqList s, MoveArgs m) {
+template <int VPR, int N>
+__global__ __launch_bounds__(256) void compact_move(PagedView v, Seqs<N> s, MoveArgs m) {
   constexpr int kPer = 4;
   const int chunk = blockIdx.x % m.chunks;
   const int rest = blockIdx.x / m.chunks;
@@ -331,14 +360,26 @@ __global__ __launch_bounds__(256) void compact_move(PagedView v, SeqList s, Move
   }
 }
 
-// f.template operator()<vectors per row>()
+template <int I>
+using Int = std::integral_constant<int, I>;
+// f(16-byte vectors of a row), f(the call's list)
 template <typename F>
 void by_row_vectors(const PagedView& v, F f) {
   switch (v.d * v.esz / 16) {
-    case 8: f(std::integral_constant<int, 8>{}); break;
-    case 16: f(std::integral_constant<int, 16>{}); break;
-    default: f(std::integral_constant<int, 32>{}); break;
+    case 8: f(Int<8>{}); break;
+    case 16: f(Int<16>{}); break;
+    default: f(Int<32>{}); break;
   }
+}
+template <typename F>
+void with_list(const SeqList& s, F f) {
+  if (s.n <= kShort) f(Seqs<kShort>(s));
+  else f(Seqs<kMaxSeqs>(s));
+}
+template <typename F>
+void with_list(const RowList& r, F f) {
+  if (r.n <= kShort) f(Rows<kShort>(r));
+  else f(Rows<kMaxSeqs>(r));
 }
 
 }  // namespace
@@ -355,7 +396,9 @@ int launch_pages_grow(const PagedView& v, const SeqList& s, const PagesWs& w, in
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   char* p = static_cast<char*>(ws);
   i32x4* info = reinterpret_cast<i32x4*>(p + w.info);
-  grow_plan<<<1, kPlanThreads, 0, st>>>(v, s, reinterpret_cast<int32_t*>(p + w.fresh), info, status);
+  with_list(s, [&](const auto& l) {
+    grow_plan<<<1, kPlanThreads, 0, st>>>(v, l, reinterpret_cast<int32_t*>(p + w.fresh), info, status);
+  });
   by_row_vectors(v, [&](auto vpr) {
     grow_copy<decltype(vpr)::value><<<dim3(s.n, v.G, v.n_layers), 256, 0, st>>>(v, info);
   });
@@ -368,20 +411,26 @@ int launch_pages_write(const PagedView& v, const RowList& r, const void* k, cons
               lay.group_stride * v.esz, lay.token_stride * v.esz};
   const int64_t nvec = (int64_t)r.row0[r.n] * v.G * (v.d * v.esz / 16);
   by_row_vectors(v, [&](auto vpr) {
-    write_kernel<decltype(vpr)::value><<<dim3((unsigned)((nvec + 255) / 256), v.n_layers), 256, 0,
-                                         reinterpret_cast<hipStream_t>(stream)>>>(v, r, a);
+    with_list(r, [&](const auto& l) {
+      write_kernel<decltype(vpr)::value><<<dim3((unsigned)((nvec + 255) / 256), v.n_layers), 256, 0,
+                                           reinterpret_cast<hipStream_t>(stream)>>>(v, l, a);
+    });
   });
   return (int)hipGetLastError();
 }
 
 int launch_pages_fork(const PagedView& v, const SeqList& s, void* stream) {
-  fork_kernel<<<s.n, 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(v, s);
+  with_list(s, [&](const auto& l) {
+    fork_kernel<<<s.n, 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(v, l);
+  });
   return (int)hipGetLastError();
 }
 
 int launch_pages_free(const PagedView& v, const SeqList& s, int keep_first, int keep_last,
                       void* stream) {
-  free_kernel<<<s.n, 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(v, s, keep_first, keep_last);
+  with_list(s, [&](const auto& l) {
+    free_kernel<<<s.n, 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(v, l, keep_first, keep_last);
+  });
   return (int)hipGetLastError();
 }
 
@@ -397,10 +446,12 @@ int launch_pages_compact(const PagedView& v, const SeqList& s, bool whole, const
   m.idx_ls = idx_ls;
   m.B = B;
   m.tail = tail;
-  compact_plan<<<1, kPlanThreads, 0, st>>>(v, s, whole, B, counts, tail,
-                                           reinterpret_cast<int32_t*>(p + w.fresh),
-                                           reinterpret_cast<i32x4*>(p + w.info),
-                                           reinterpret_cast<int32_t*>(p + w.old), status);
+  with_list(s, [&](const auto& l) {
+    compact_plan<<<1, kPlanThreads, 0, st>>>(v, l, whole, B, counts, tail,
+                                             reinterpret_cast<int32_t*>(p + w.fresh),
+                                             reinterpret_cast<i32x4*>(p + w.info),
+                                             reinterpret_cast<int32_t*>(p + w.old), status);
+  });
   if (B + tail > 0) {
     // the most rows of a sequence: the kept ones and the first page's before them
     const int vpr_n = v.d * v.esz / 16;
@@ -409,7 +460,9 @@ int launch_pages_compact(const PagedView& v, const SeqList& s, bool whole, const
     const int64_t most = std::max<int64_t>(1, (int64_t)INT32_MAX / per);
     m.chunks = (int)std::min<int64_t>({(nvec + 1023) / 1024, most, 65535});
     by_row_vectors(v, [&](auto vpr) {
-      compact_move<decltype(vpr)::value><<<(unsigned)(per * m.chunks), 256, 0, st>>>(v, s, m);
+      with_list(s, [&](const auto& l) {
+        compact_move<decltype(vpr)::value><<<(unsigned)(per * m.chunks), 256, 0, st>>>(v, l, m);
+      });
     });
   }
   return (int)hipGetLastError();
