@@ -300,25 +300,33 @@ def test_infinities_and_nan_in_masked_places(dtype, d, T):
         run(f"{bad} tree", c, mask=tree_masks(c.r, [T, T], 1), lse=False)
 
 
-def test_lowest_and_largest_logits():
-    """Logits near the type's limits stay apart from masked ones."""
-    c = Case(15, [50], [3], 4, 2, 64, 16, "f32")
-    p, row = c.m.at(c.slots[0], 10)
+@pytest.mark.parametrize("dtype,T", [("f32", 3), ("f32", 40), ("bf16", 3), ("bf16", 40)])
+def test_logits_near_the_largest(dtype, T):
+    """Logits near float32's limits stay apart from masked ones, and their
+    differences count though no float32 multiple of them by the scale would
+    keep them: equal weights over the multiples of 7 that a row sees, none
+    elsewhere."""
+    c = Case(15, [50], [T], 4, 2, 64, 16, dtype)
+    k = np.zeros(64)
     for t in range(50):
         p, row = c.m.at(c.slots[0], t)
-        c.m.k[0, p, :, row] = 0
-        c.m.k[0, p, :, row, 0] = -3e37 if t % 7 else -2.9e37
-    c.q[...] = 0
-    c.q[..., 0] = 8.0
+        k[0] = -3e37 if t % 7 else -2.9e37
+        c.m.k[0, p, :, row] = to_store(k, dtype)
+    q = np.zeros(64)
+    q[0] = 8.0
+    c.q[...] = to_store(q, dtype)
     c.upload()
     c.call()
     torch.cuda.synchronize()
-    # equal weights over the multiples of 7 that each row sees
-    v = np.stack([c.m.v[0, c.m.at(c.slots[0], t)[0], :, c.m.at(c.slots[0], t)[1]] for t in range(0, 50, 7)])
-    for i, n in enumerate((7, 7, 8)):
-        want = v[:n].astype(np.float64).mean(0)          # [G, d]; head h of group h // 2
+    f = to_f64(dtype)
+    v = np.stack([f(c.m.v[0, c.m.at(c.slots[0], t)[0], :, c.m.at(c.slots[0], t)[1]])
+                  for t in range(0, 50, 7)])
+    for i in range(T):
+        n = (50 - T + i) // 7 + 1
+        want = v[:n].mean(0).repeat(2, 0)                 # head h is of group h // 2
         got = c.out[i].double().cpu().numpy()
-        assert np.abs(got - want.repeat(2, 0)).max() <= 64 * U * np.abs(v).max()
+        low = 2.0 ** -8 * np.abs(want) if dtype == "bf16" else 0
+        assert np.all(np.abs(got - want) <= low + 64 * U * np.abs(v).max()), i
 
 
 def test_splits_and_short_bounds():
@@ -417,3 +425,38 @@ def test_captured_calls_follow_the_lengths():
         c.lse[sum(c.rows):] = 7
         c.check(f"replay tree {lens}", mask=mask)
         c.out, c.lse = keep
+
+
+def test_the_binding_refuses():
+    c = Case(22, [40], [2], 4, 2, 64, 16)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    call = lambda q=c.qd, out=c.out, rows=(2,), lse=None, w=ws: pg.attend_window(
+        c.c, c.slots, list(rows), q, 0, 0, out, w, lse=lse, max_len=40)
+    with pytest.raises(ValueError, match="q: torch.float32"):
+        call(q=c.qd.float())
+    with pytest.raises(ValueError, match="contiguous"):
+        call(q=c.qd.transpose(1, 2))
+    with pytest.raises(ValueError, match="out"):
+        call(out=c.out[:1])
+    with pytest.raises(ValueError, match="device tensor"):
+        call(out=c.out.cpu())
+    with pytest.raises(ValueError, match="one number per slot"):
+        call(rows=(1, 1))
+    with pytest.raises(ValueError, match="lse"):
+        call(lse=c.lse.double())
+    with pytest.raises(ValueError, match="mask"):
+        pg.attend_tree(c.c, c.slots, [2], c.qd, torch.zeros(1, 1, dtype=torch.int64, device="cuda"),
+                       c.out, ws)
+    with pytest.raises(pg.StarKVError, match="E_PARAM"):
+        call(rows=(1 << 20,), q=torch.empty(1, dtype=c.qd.dtype, device="cuda").expand(
+            1 << 28).contiguous(), out=torch.empty(1 << 28, dtype=c.qd.dtype, device="cuda"))
+    with pytest.raises(ValueError, match="strides"):
+        pg.Cache(c.c.k, c.c.v.transpose(0, 1).contiguous(), c.c.table, c.c.length, c.c.refs, 4)
+    with pytest.raises(ValueError, match="refs"):
+        pg.Cache(c.c.k, c.c.v, c.c.table, c.c.length, c.c.refs[:-1], 4)
+    with pytest.raises(ValueError, match="idx"):
+        pg.pages_compact(c.c, c.slots, torch.zeros(3, 1, 2, dtype=torch.int32, device="cuda"),
+                         torch.zeros(1, dtype=torch.int32, device="cuda"), ws)
+    call()                                    # and takes the call that is right
+    torch.cuda.synchronize()
+    c.check("right", lse=False)
