@@ -174,16 +174,24 @@ __global__ __launch_bounds__(kThreads) void attend_few(PagedView v, AttendArgs a
   const const_i32* table = const_ints(v.table + (size_t)s.r.slot[b] * v.max_pages);
   const int64_t base = (int64_t)layer * v.ls + (int64_t)g * v.gs;
   const int u1 = min((split + 1) * ts.per, ts.nt);
-  for (int u = split * ts.per + wave; u < u1; u += kWaves) {
+  // the page of a step's 16-token half, read a step before its use
+  const auto page_of = [&](int u, int h) {
+    const int t = step_token<kStep>(ts, min(u, ts.nt - 1)) + 16 * h;
+    return table[min(t, ts.n - 1) >> v.psh];
+  };
+  int u = split * ts.per + wave, next0 = 0, next1 = 0;
+  if (u < u1) {
+    next0 = page_of(u, 0);
+    next1 = page_of(u, 1);
+  }
+  for (; u < u1; u += kWaves) {
     const int t0 = step_token<kStep>(ts, u);
-    // the two 16-token halves of a step lie in one page each; where there is
-    // no page the loads go to page 0 and the tokens are masked below
-    int page[2];
+    // where there is no page the loads go to page 0 and the tokens are masked
+    // below
+    int page[2] = {next0, next1};
     bool there[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int t = t0 + 16 * h;
-      page[h] = t < ts.n ? table[t >> v.psh] : -1;
       there[h] = page[h] >= 0 && page[h] < v.n_pages;
       if (!there[h]) page[h] = 0;
     }
@@ -203,6 +211,8 @@ __global__ __launch_bounds__(kThreads) void attend_few(PagedView v, AttendArgs a
         for (int c = 0; c < VR::kLoads; ++c)
           vv[4 * h + j][c] = *reinterpret_cast<const vrow*>(vr + j * v.ts + 16 * sizeof(vrow) * c);
     }
+    next0 = page_of(u + kWaves, 0);
+    next1 = page_of(u + kWaves, 1);
     const bool whole = there[0] && there[1] && sees_step<kStep>(all, t0);
 
     f32x4 x[NB][2];
