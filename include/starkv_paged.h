@@ -77,7 +77,8 @@ typedef struct starkv_paged {
 /* What grow and compact report per sequence of the call (int32, device). */
 #define STARKV_SEQ_OK 0
 #define STARKV_SEQ_NO_PAGES 1  /* the pool had too few free pages: unchanged */
-#define STARKV_SEQ_RANGE 2     /* past the table row, or tail past the sequence: unchanged */
+#define STARKV_SEQ_RANGE 2     /* past the table row, tail past the sequence, or it would go on
+                                  within a page that was dropped: unchanged */
 
 /* ------------------------------------------------------------------ */
 /* pages                                                               */
@@ -111,7 +112,8 @@ starkv_status starkv_pages_grow(const starkv_paged* cache, const int32_t* slots,
  * r of k and v, layout *rows_layout with "token" the row number over all
  * sequences of the call in order, group the KV group.  Tokens without a page,
  * of a page that another sequence shares, or before the sequence's first are
- * not written.  k, v: device, the cache's dtype.
+ * not written.  (After a grow that left a sequence unchanged, its last tokens
+ * are older ones.)  k, v: device, the cache's dtype.
  * Errors: E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_PARAM, E_HIP. */
 starkv_status starkv_pages_write(const starkv_paged* cache, const int32_t* slots, int32_t n,
                                  const int32_t* rows, const void* k, const void* v,

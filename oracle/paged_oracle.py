@@ -58,7 +58,10 @@ class PagedModel:
                 status.append(OK)
                 continue
             old = int(self.table[b, have - 1]) if part else -1
-            replace = part > 0 and (not self.is_page(old) or first[old] > 1)
+            if part and not self.is_page(old):
+                status.append(RANGE)
+                continue
+            replace = part > 0 and first[old] > 1
             need = self.pages(n + a) - have + (1 if replace else 0)
             got = None if short and need else self._take(free, need)
             if got is None:
@@ -68,7 +71,7 @@ class PagedModel:
             col = have - 1 if replace else have
             self.table[b, col:col + need] = got
             self.refs[got] = 1
-            if replace and self.is_page(old):
+            if replace:
                 for x in (self.k, self.v):
                     x[:, got[0], :, :part] = x[:, old, :, :part]
                 self.refs[old] -= 1
@@ -125,7 +128,8 @@ class PagedModel:
             a, B = n - s, idx.shape[2]
             cnt = B if counts is None else min(max(int(counts[i]), 0), B)
             new = a + cnt + tail
-            if tail > s or new > self.cap:
+            gone = cnt + tail > 0 and a % self.P and not self.is_page(self.table[b, a // self.P])
+            if tail > s or new > self.cap or gone:
                 status.append(RANGE)
                 continue
             col = a // self.P if cnt + tail else self.pages(a)

@@ -119,14 +119,15 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan(PagedView v, Seqs<N> s
     } else if (add > 0) {
       len1 = (int)to;
       if (part) {
-        // the partly filled last page: replaced where it is shared or gone
+        // the partly filled last page: replaced where it is shared.  Where it
+        // was dropped there is no page to go on in: a fresh one would bring
+        // back the dropped tokens, with rows that nobody wrote
         old = table_row(v, s.slot[b])[col - 1];
-        const bool there = is_page(v, old);
-        if (!there || v.refs[old] > 1) --col;
+        if (!is_page(v, old)) st = STARKV_SEQ_RANGE;
+        else if (v.refs[old] > 1) --col;
         else old = -1;
-        if (!there) old = -1;
       }
-      need = pages_of(v, to) - col;
+      if (st == STARKV_SEQ_OK) need = pages_of(v, to) - col;
     } else {
       len1 = len0;
     }
@@ -252,7 +253,10 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan(PagedView v, Seqs<N
     a = len0 - span;
     cnt = counts ? min(max(counts[b], 0), B) : B;
     const int64_t to = (int64_t)a + cnt + tail;
-    if (tail > span || to > v.cap) {
+    // token a's page keeps the tokens before a: not where it was dropped
+    const bool gone = cnt + tail > 0 && (a & (v.P - 1)) &&
+                      !is_page(v, table_row(v, s.slot[b])[a >> v.psh]);
+    if (tail > span || to > v.cap || gone) {
       st = STARKV_SEQ_RANGE;
     } else {
       len1 = (int)to;

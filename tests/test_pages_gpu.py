@@ -156,7 +156,7 @@ def test_grow_serves_in_order_while_pages_last():
     assert list(b.grow([4], [32])) == [0]
 
 
-def test_dropped_last_page_is_replaced_and_bad_entries_are_no_pages():
+def test_bad_entries_are_no_pages():
     b = Both()
     b.grow([0], [40])
     b.write([0], [40])
@@ -168,9 +168,27 @@ def test_dropped_last_page_is_replaced_and_bad_entries_are_no_pages():
     b.c.refs.copy_(torch.from_numpy(b.m.refs))
     b.write([0], [40])                    # only the middle page's rows
     b.fork([0], [1])
-    b.grow([1], [1])                      # its last page is none: a fresh one, nothing copied
+    assert list(b.grow([1], [1])) == [2]  # its last page is none
     b.compact([0], np.arange(40, dtype=np.int32)[None, None, ::5].copy(), tail=0)
     b.free([0, 1])
+
+
+def test_no_sequence_goes_on_within_a_dropped_page():
+    """Back to a length whose last page the window let go: what was dropped
+    stays dropped, so the page's further rows cannot be used."""
+    b = Both(n_pages=40)
+    for n in (40, 48):                              # within a dropped page, and at its end
+        b.grow([0, 1], [100, 100])
+        b.write([0, 1], [100, 100])
+        b.free([0, 1], first=4, last=30)            # pages 1 to 3
+        idx = np.zeros((1, 2, 3), dtype=np.int32)
+        bad = 2 if n % 16 else 0
+        assert list(b.compact([0, 1], idx, span=[100 - n, 20])) == [bad, 0]
+        b.free([0], first=n)
+        assert list(b.grow([0, 1], [9, 9])) == [bad, 0]
+        assert list(b.grow([0], [0])) == [0]
+        assert list(b.compact([0], np.zeros((1, 1, 0), dtype=np.int32), span=[0])) == [0]
+        b.free([0, 1])
 
 
 @pytest.mark.parametrize("dtype,d,P", [("bf16", 128, 16), ("f32", 64, 64), ("bf16", 64, 32),
