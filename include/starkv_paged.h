@@ -163,7 +163,10 @@ starkv_status starkv_pages_compact(const starkv_paged* cache, const int32_t* slo
 /* ------------------------------------------------------------------ */
 /* Both calls take rows[b] >= 0 query tokens (host) of each sequence (a slot
  * may repeat): those of its last rows[b] cached tokens, whose K and V are in
- * the cache already.  With V(i) the cached tokens that query token i sees,
+ * the cache already.  rows[b] is at most what a table row holds, their sum at
+ * most 2^26, and n_layers * G * sum of ceil(rows[b]*H/G / 16) at most 2^23
+ * (E_PARAM; bf16 calls of many rows take eight times as many).  With V(i) the
+ * cached tokens that query token i sees,
  *   x[h,t] = q[h] . K[g(h),t] / sqrt(d),
  *   out[h] = sum_{t in V(i)} softmax_t(x[h,t]) V[g(h),t],
  *   lse[h] = ln sum_{t in V(i)} exp(x[h,t]).

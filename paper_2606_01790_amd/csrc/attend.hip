@@ -478,8 +478,10 @@ int launch(const PagedView& v, const AttendArgs& a, const AttendLists& l, const 
     const int handfuls = s.row_tile / (kSlots / groups);
     const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(handfuls, 2048 / s.units));
     const unsigned joins = (unsigned)(s.units * parts);
-    if (s.many) attend_join<T, D, 64><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile, groups, parts);
-    else attend_join<T, D, kStep><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile, groups, parts);
+    if (!s.many)
+      attend_join<T, D, kStep><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile, groups, parts);
+    else if constexpr (sizeof(T) == 2)
+      attend_join<T, D, 64><<<joins, kThreads, 0, st>>>(v, a, l, s.row_tile, groups, parts);
   }
   return (int)hipGetLastError();
 }

@@ -45,7 +45,7 @@ starkv_status check_paged(const starkv_paged* c, PagedView* v);
 // n slots of the cache, each at most once if `once`.
 starkv_status check_slots(const PagedView& v, const int32_t* slots, int32_t n, bool once);
 
-// Workspace of grow and compact, in int32 units: the free pages found, the
+// Workspace of grow and compact, byte offsets: the free pages found, the
 // pages to copy (grow) or the sequences' extents (compact), and the table
 // rows as they were (compact).
 struct PagesWs {

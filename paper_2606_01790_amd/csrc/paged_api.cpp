@@ -2,7 +2,6 @@
 // an attention call into blocks, then the kernels' launch functions.  Nothing
 // here allocates memory or synchronises a stream.
 #include <algorithm>
-#include <climits>
 
 #include "paged.h"
 
@@ -139,13 +138,17 @@ int split_count(const AttendShape& s, int n, int d, int64_t steps, int64_t most)
   // end are worth; joining costs two steps and one per 10 MB of partial sums
   double best = 0;
   int best_ns = 1;
-  for (int64_t ns = 1; ns <= std::min<int64_t>(top, std::max<int64_t>(1, 4096 / s.units)); ++ns) {
-    double cost = (double)((s.units * ns + 511) / 512) * (double)((steps + ns - 1) / ns + 4);
+  const int64_t last = std::min<int64_t>(top, std::max<int64_t>(1, 4096 / s.units));
+  for (int64_t ns = 1; ns <= last;) {
+    const int64_t per = (steps + ns - 1) / ns;
+    double cost = (double)((s.units * ns + 511) / 512) * (double)(per + 4);
     if (ns > 1) cost += 2 + (double)(s.units * ns) * s.row_tile * d * 8 / 10e6;
     if (ns == 1 || cost < best) {
       best = cost;
       best_ns = (int)ns;
     }
+    if (per == 1) break;
+    ns = (steps + per - 2) / (per - 1);   // the least with shorter splits; between them none is cheaper
   }
   return best_ns;
 }
@@ -187,7 +190,9 @@ starkv_status attend_shape(const PagedView& v, const int32_t* rows, int n, int32
   const int64_t steps = std::max<int64_t>(1, (seen + step - 1) / step);
   s->n_split = split_count(*s, n, v.d, steps, most_split);
   s->chunk = (int)((steps + s->n_split - 1) / s->n_split * step);
-  if (tiles > INT32_MAX || s->units * most_split > INT32_MAX / 16) return STARKV_E_PARAM;
+  // (up to 1.6 blocks to a tile's split, each of 256 of a launch's 2^32
+  // threads; and a sequence's rows stay below 2^31)
+  if (s->units > 1 << 23) return STARKV_E_PARAM;
   s->n_tiles = (int)tiles;
   s->stat_off = s->steps_off = s->ws_bytes = 0;
   s->steps = (int)steps;

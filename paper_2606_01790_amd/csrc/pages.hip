@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kScan = 8;          // reference counts per thread of a scan step
+constexpr int64_t kMaxBlocks = (1 << 24) - 1;   // of 256 threads: a launch has under 2^32 of them
 
 __device__ inline bool is_page(const PagedView& v, int32_t p) { return p >= 0 && p < v.n_pages; }
 __device__ inline int seq_len(const PagedView& v, int slot) {
@@ -178,25 +179,28 @@ struct WriteArgs {
   int64_t ls, gs, ts;   // byte strides
 };
 
-// One 16-byte vector of K and V per thread.  The page of a token must belong
-// to its sequence alone: a shared one is left as it is.
+// 16-byte vectors of K and V, one per thread (or, where a launch cannot hold
+// as many threads, several).  The page of a token must belong to its sequence
+// alone: a shared one is left as it is.
 template <int VPR, int N>
 __global__ __launch_bounds__(256) void write_kernel(PagedView v, Rows<N> r, WriteArgs a) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int part = (int)(i % VPR);
-  const int64_t rg = i / VPR;
-  const int g = (int)(rg % v.G), row = (int)(rg / v.G), layer = blockIdx.y;
-  if (row >= r.row0[r.n]) return;
-  const int b = owner_of(r.row0, r.n, row);
-  const int t = seq_len(v, r.slot[b]) - r.row0[b + 1] + row;
-  if (t < 0) return;
-  const int page = table_row(v, r.slot[b])[t >> v.psh];
-  if (!is_page(v, page) || v.refs[page] > 1) return;
-  const int64_t from = (int64_t)layer * a.ls + (int64_t)g * a.gs + (int64_t)row * a.ts + part * 16;
-  const int64_t to = (int64_t)layer * v.ls + (int64_t)page * v.ps + (int64_t)g * v.gs +
-                     (int64_t)(t & (v.P - 1)) * v.ts + part * 16;
-  *reinterpret_cast<i32x4*>(v.k + to) = *reinterpret_cast<const i32x4*>(a.k + from);
-  *reinterpret_cast<i32x4*>(v.v + to) = *reinterpret_cast<const i32x4*>(a.v + from);
+  const int64_t n = (int64_t)r.row0[r.n] * v.G * VPR;
+  const int layer = blockIdx.y;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int part = (int)(i % VPR);
+    const int64_t rg = i / VPR;
+    const int g = (int)(rg % v.G), row = (int)(rg / v.G);
+    const int b = owner_of(r.row0, r.n, row);
+    const int t = seq_len(v, r.slot[b]) - r.row0[b + 1] + row;
+    if (t < 0) continue;
+    const int page = table_row(v, r.slot[b])[t >> v.psh];
+    if (!is_page(v, page) || v.refs[page] > 1) continue;
+    const int64_t from = (int64_t)layer * a.ls + (int64_t)g * a.gs + (int64_t)row * a.ts + part * 16;
+    const int64_t to = (int64_t)layer * v.ls + (int64_t)page * v.ps + (int64_t)g * v.gs +
+                       (int64_t)(t & (v.P - 1)) * v.ts + part * 16;
+    *reinterpret_cast<i32x4*>(v.k + to) = *reinterpret_cast<const i32x4*>(a.k + from);
+    *reinterpret_cast<i32x4*>(v.v + to) = *reinterpret_cast<const i32x4*>(a.v + from);
+  }
 }
 
 // Sequence s.slot[b] becomes a fork of s.num[b], one pair per block.  No
@@ -318,7 +322,7 @@ template <int VPR, int N>
 __global__ __launch_bounds__(256) void compact_move(PagedView v, Seqs<N> s, MoveArgs m) {
   const int chunk = blockIdx.x % m.chunks;
   const int rest = blockIdx.x / m.chunks;
-  const int g = rest % v.G, b = rest / v.G % s.n, layer = rest / v.G / s.n;
+  const int g = rest % v.G, b = rest / v.G, layer = blockIdx.y;
   const i32x4 info = m.info[b];
   const int len0 = info[0], a = info[1], cnt = info[2];
   if (cnt < 0) return;
@@ -401,10 +405,11 @@ int launch_pages_write(const PagedView& v, const RowList& r, const void* k, cons
   WriteArgs a{static_cast<const char*>(k), static_cast<const char*>(vv), lay.layer_stride * v.esz,
               lay.group_stride * v.esz, lay.token_stride * v.esz};
   const int64_t nvec = (int64_t)r.row0[r.n] * v.G * (v.d * v.esz / 16);
+  const unsigned blocks = (unsigned)std::min((nvec + 255) / 256, kMaxBlocks);
   by_row_vectors(v, [&](auto vpr) {
     with_list(r, [&](const auto& l) {
-      write_kernel<decltype(vpr)::value><<<dim3((unsigned)((nvec + 255) / 256), v.n_layers), 256, 0,
-                                           reinterpret_cast<hipStream_t>(stream)>>>(v, l, a);
+      write_kernel<decltype(vpr)::value>
+          <<<dim3(blocks, v.n_layers), 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(v, l, a);
     });
   });
   return (int)hipGetLastError();
@@ -447,12 +452,12 @@ int launch_pages_compact(const PagedView& v, const SeqList& s, bool whole, const
     // the most rows of a sequence: the kept ones and the first page's before them
     const int vpr_n = v.d * v.esz / 16;
     const int64_t nvec = ((int64_t)B + tail + v.P - 1) * vpr_n;
-    const int64_t per = (int64_t)v.n_layers * s.n * v.G;
-    const int64_t most = std::max<int64_t>(1, (int64_t)INT32_MAX / per);
-    m.chunks = (int)std::min<int64_t>({(nvec + 255) / 256, most, 65535});
+    const int64_t per = (int64_t)s.n * v.G;      // at most 2^14
+    m.chunks = (int)std::min<int64_t>({(nvec + 255) / 256, kMaxBlocks / per, 65535});
     by_row_vectors(v, [&](auto vpr) {
       with_list(s, [&](const auto& l) {
-        compact_move<decltype(vpr)::value><<<(unsigned)(per * m.chunks), 256, 0, st>>>(v, l, m);
+        compact_move<decltype(vpr)::value>
+            <<<dim3((unsigned)(per * m.chunks), v.n_layers), 256, 0, st>>>(v, l, m);
       });
     });
   }

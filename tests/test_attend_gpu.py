@@ -215,6 +215,15 @@ def test_row_counts(rows, H, G, d):
     run("window", c, window=50, sinks=5)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,T", [(300, 1, 2), (129, 1, 1), (320, 2, 3), (64, 64, 17)])
+def test_heads_of_a_group(H, G, T, dtype):
+    """More heads to a group than a block takes rows, and as few as one."""
+    c = Case(31 + H, [70, 5], [T, 1], H=H, G=G, d=64, P=16, dtype=dtype)
+    run(f"H {H} G {G} T {T} {dtype}", c, mask=tree_masks(c.r, c.rows, 1))
+    run(f"H {H} G {G} T {T} {dtype} window", c, window=9, sinks=2)
+
+
 @pytest.mark.parametrize("n", [1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511,
                                513, 1500])
 def test_lengths(n):

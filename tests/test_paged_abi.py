@@ -241,6 +241,21 @@ def test_attention_arguments():
     assert L.starkv_attend_workspace_bytes(r, ints([8]), 1, 0) == 0
 
 
+def test_attention_of_more_rows_than_a_launch_holds():
+    L = pg.lib()
+    # 28 layers, 4 groups of 7 heads: 2^23 / 112 tiles of 128 rows, of 16 in float32
+    for dtype, tile in ((sk.BF16, 128), (sk.F32, 16)):
+        c = ctypes.byref(cache(dtype=dtype, max_pages=1 << 20))
+        most = (1 << 23) // 112 * tile // 7
+        for rows in ([most + tile], [1] * 255 + [most]):
+            assert name(L.starkv_attend_window(c, ints([1] * len(rows)), len(rows), ints(rows), FAKE, 0,
+                                               0, 1 << 20, FAKE, None, FAKE, BIG, None)) == "E_PARAM"
+    # one layer of one group of 64 heads: 2^26 tokens are 2^32 rows
+    c = ctypes.byref(cache(n_layers=1, H=64, G=1, max_pages=1 << 20))
+    assert name(L.starkv_attend_window(c, ints([1]), 1, ints([1 << 26]), FAKE, 0, 0, 1, FAKE, None, FAKE,
+                                       BIG, None)) == "E_PARAM"
+
+
 def test_the_binding_refuses_host_tensors():
     k = torch.zeros(1, 4, 2, 16, 64, dtype=torch.bfloat16)
     i = lambda *s: torch.zeros(*s, dtype=torch.int32)

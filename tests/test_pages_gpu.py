@@ -282,6 +282,32 @@ def test_many_sequences_and_a_large_pool():
     b.grow(slots[::2][100:120], [3] * 20)
 
 
+def test_calls_of_more_threads_than_a_launch_holds():
+    """A sequence of 2^26 tokens, all but its last page dropped: over 2^32 vectors
+    to write in each layer, of one row that stands for all, and a list of 2^22
+    tokens to keep, of which three count."""
+    G, P, d, most = 64, 1024, 64, 1 << 16
+    b = Both(nl=5, G=G, H=G, P=P, d=d, n_pages=4, n_slots=1, max_pages=most)
+    b.m.len[0] = most * P
+    b.m.table[0, -1], b.m.refs[2] = 2, 1
+    b.c.table.copy_(torch.from_numpy(b.m.table))
+    b.c.length.copy_(torch.from_numpy(b.m.len))
+    b.c.refs.copy_(torch.from_numpy(b.m.refs))
+    row = torch.arange(d, dtype=torch.int16, device="cuda").view(torch.bfloat16)
+    pg.pages_write(b.c, [0], [(1 << 23) + 1000], row, row, pg.KVLayout(0, 0, 0))
+    b.m.k[:, 2] = b.m.v[:, 2] = np.arange(d)
+    b.check("write")
+    idx = torch.zeros(1, 1, 1 << 22, dtype=torch.int32, device="cuda")
+    idx[0, 0, 2] = 9
+    ws = torch.empty(pg.pages_workspace_bytes(b.c, 1, 1 << 22), dtype=torch.uint8, device="cuda")
+    status = torch.full((1,), 9, dtype=torch.int32, device="cuda")
+    pg.pages_compact(b.c, [0], idx, status, ws, span=[P],
+                     counts=torch.tensor([3], dtype=torch.int32, device="cuda"))
+    assert list(b.m.compact([0], np.array([[[0, 0, 9]]], dtype=np.int32), span=[P])) == [0]
+    b.check("compact")
+    assert int(status) == 0
+
+
 def test_a_captured_step_replays():
     """Fork, grow, write and compact in one graph, replayed with eager work
     and synchronizations between: each replay is the eager call's result."""
