@@ -115,16 +115,21 @@ namespace {
 
 // How many splits a (layer, group, row tile)'s steps are divided into, at
 // most `most`, in a call of n sequences.
-int split_count(const AttendShape& s, int n, int d, int64_t steps, int64_t most) {
+int split_count(const AttendShape& s, int n, int d, int esz, int64_t steps, int64_t most) {
   if (s.units == 0) return 1;
   if (!s.many) {
     // bound by HBM: splits of at least two steps for each of a block's waves
-    // (four in the kernel for 32 rows, whose blocks take longer to end), and
-    // no more than some 1,024 blocks.  Measured, 256 against 512 tokens: one
-    // sequence of 13,711 tokens 13.7 and 15.6 us, eight trees of four tokens
-    // (28 rows) 47.8 and 34.3
+    // (four in the kernel for 32 rows, whose blocks take longer to end).
+    // Measured, 256 against 512 tokens: one sequence of 13,711 tokens 13.7 and
+    // 15.6 us, eight trees of four tokens (28 rows) 47.8 and 34.3
     const int64_t least = s.row_tile == 32 ? 16 : 8;
-    const int64_t ns = std::min((steps + least - 1) / least, std::max<int64_t>(1, 1024 / s.units));
+    // and of so many blocks in all that each CU has two, which keep HBM busy;
+    // float32, bound by its matrix instructions, takes twice as many, which
+    // come out more even.  512 against 1,024 blocks: 28 layers of 4 trees of 4
+    // tokens 127 and 145 us, 64 sequences of one token 94 and 103, 12 of 3,000
+    // to 9,000 tokens 59 and 54; float32 trees of up to 13 tokens 62 and 39
+    const int64_t blocks = esz == 2 ? 512 : 1024;
+    const int64_t ns = std::min((steps + least - 1) / least, std::max<int64_t>(1, blocks / s.units));
     return (int)std::max<int64_t>(1, std::min(ns, most));
   }
   const int64_t top = std::min(steps, most);
@@ -183,12 +188,12 @@ starkv_status attend_shape(const PagedView& v, const int32_t* rows, int n, int32
   // of a call without a window, whose splits bound those of one with it.
   const int64_t len = std::min<int64_t>(max_len, v.cap);
   const int step = s->many ? 64 : 32;
-  const int most_split = split_count(*s, n, v.d, (len + step - 1) / step, INT32_MAX);
+  const int most_split = split_count(*s, n, v.d, v.esz, (len + step - 1) / step, INT32_MAX);
   const int64_t row_tokens = (s->row_tile + hpg - 1) / hpg + 1;
   const int64_t seen = window ? std::min<int64_t>(len, (int64_t)window + sinks + row_tokens + 2 * step)
                               : len;
   const int64_t steps = std::max<int64_t>(1, (seen + step - 1) / step);
-  s->n_split = split_count(*s, n, v.d, steps, most_split);
+  s->n_split = split_count(*s, n, v.d, v.esz, steps, most_split);
   s->chunk = (int)((steps + s->n_split - 1) / s->n_split * step);
   // (up to 1.6 blocks to a tile's split, each of 256 of a launch's 2^32
   // threads; and a sequence's rows stay below 2^31)
