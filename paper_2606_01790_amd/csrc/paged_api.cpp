@@ -129,7 +129,14 @@ int split_count(const AttendShape& s, int n, int d, int esz, int64_t steps, int6
     // tokens 127 and 145 us, 64 sequences of one token 94 and 103, 12 of 3,000
     // to 9,000 tokens 59 and 54; float32 trees of up to 13 tokens 62 and 39
     const int64_t blocks = esz == 2 ? 512 : 1024;
-    const int64_t ns = std::min((steps + least - 1) / least, std::max<int64_t>(1, blocks / s.units));
+    // of several sequences, whose lengths may be far from each other, none of
+    // over 3,200 tokens (float32: 1,536), or one long sequence would hold up
+    // the rest (28 layers of five sequences of 1,000 to 5,000 tokens 241 us
+    // without and 234 with; float32, eight trees over 1,664 to 39,197 tokens
+    // 437 and 370)
+    const int64_t longest = esz == 2 ? 100 : 48;
+    const int64_t even = n > 1 ? (steps + longest - 1) / longest : 1;
+    const int64_t ns = std::min((steps + least - 1) / least, std::max(even, blocks / s.units));
     return (int)std::max<int64_t>(1, std::min(ns, most));
   }
   const int64_t top = std::min(steps, most);
