@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kScan = 8;          // reference counts per thread of a scan step
+constexpr int kLowFresh = 1024;   // fresh pages kept in LDS
 constexpr int64_t kMaxBlocks = (1 << 24) - 1;   // of 256 threads: a launch has under 2^32 of them
 
 __device__ inline bool is_page(const PagedView& v, int32_t p) { return p >= 0 && p < v.n_pages; }
@@ -70,26 +71,65 @@ __device__ inline int owner_of(const int32_t* first, int n, int k) {
   return lo;
 }
 
-// The lowest `total` free pages, ascending, into fresh[]; how many there are.
-__device__ int take_pages(const PagedView& v, int total, int32_t* fresh, int* sh) {
-  int found = 0;
-  for (int base = 0; base < v.n_pages && found < total; base += kPlanThreads * kScan) {
-    const int p0 = base + (int)threadIdx.x * kScan;
-    unsigned m = 0;
+// Which of the kScan pages from p0 on are free, bit by bit.
+__device__ inline unsigned free_pages(const PagedView& v, int p0) {
+  unsigned m = 0;
 #pragma unroll
-    for (int j = 0; j < kScan; ++j)
-      if (p0 + j < v.n_pages && v.refs[p0 + j] == 0) m |= 1u << j;
-    int tot;
-    int r = found + block_excl_scan(__popc(m), sh, &tot);
+  for (int j = 0; j < kScan; ++j)
+    if (p0 + j < v.n_pages && v.refs[p0 + j] == 0) m |= 1u << j;
+  return m;
+}
+
+// The fresh pages of a call, the first in LDS and the rest in the workspace.
+struct Fresh {
+  int32_t* low;
+  int32_t* rest;
+  __device__ inline void put(int i, int page) const {
+    if (i < kLowFresh) low[i] = page;
+    else rest[i] = page;
+  }
+  __device__ inline int at(int i) const { return i < kLowFresh ? low[i] : rest[i]; }
+};
+
+// The pages that the sequences need, thread b's `need` behind those of the
+// threads before it, *excl: the lowest free ones, ascending.  Returns how many
+// there are, at most what is needed.  `m`: the thread's first free_pages, read
+// while the needs were worked out and counted with them.
+__device__ int take_pages(const PagedView& v, int need, unsigned m, const Fresh& fresh, int (*sh)[2],
+                          int* excl) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int inc0 = wave_incl_scan(need), inc1 = wave_incl_scan(__popc(m));
+  if (lane == 63) {
+    sh[w][0] = inc0;
+    sh[w][1] = inc1;
+  }
+  __syncthreads();
+  int before0 = 0, before1 = 0, total = 0, tot = 0;
+#pragma unroll
+  for (int i = 0; i < kPlanThreads / 64; ++i) {
+    if (i < w) {
+      before0 += sh[i][0];
+      before1 += sh[i][1];
+    }
+    total += sh[i][0];
+    tot += sh[i][1];
+  }
+  *excl = before0 + inc0 - need;
+  int r = before1 + inc1 - __popc(m), found = 0, base = 0;
+  for (;;) {
     while (m) {
       const int j = __ffs(m) - 1;
       m &= m - 1;
-      if (r < total) fresh[r] = p0 + j;
+      if (r < total) fresh.put(r, base + (int)threadIdx.x * kScan + j);
       ++r;
     }
     found += tot;
+    base += kPlanThreads * kScan;
+    if (found >= total || base >= v.n_pages) break;
+    m = free_pages(v, base + (int)threadIdx.x * kScan);
+    r = found + block_excl_scan(__popc(m), &sh[0][0], &tot);
   }
-  __syncthreads();   // fresh[] is read by other threads of the block
+  __syncthreads();   // the fresh pages are read by other threads of the block
   return min(found, total);
 }
 
@@ -105,10 +145,13 @@ __global__ __launch_bounds__(256) void init_kernel(PagedView v) {
 // Pages for the new tokens.  info[b]: the page to copy from (or -1), to, and
 // the rows to copy.
 template <int N>
-__global__ __launch_bounds__(kPlanThreads) void grow_plan(PagedView v, Seqs<N> s, int32_t* fresh,
+__global__ __launch_bounds__(kPlanThreads) void grow_plan(PagedView v, Seqs<N> s, int32_t* rest,
                                                           i32x4* info, int32_t* status) {
-  __shared__ int pre[kMaxSeqs], first[kMaxSeqs], ok[kMaxSeqs], sh[kPlanThreads / 64];
+  __shared__ int pre[kMaxSeqs], first[kMaxSeqs], ok[kMaxSeqs], sh[kPlanThreads / 64][2];
+  __shared__ int32_t low[kLowFresh];
+  const Fresh fresh{low, rest};
   const int b = threadIdx.x;
+  const unsigned free0 = free_pages(v, b * kScan);
   int need = 0, col = 0, part = 0, st = STARKV_SEQ_OK, old = -1, len1 = 0;
   if (b < s.n) {
     const int len0 = seq_len(v, s.slot[b]), add = s.num[b];
@@ -133,9 +176,8 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan(PagedView v, Seqs<N> s
       len1 = len0;
     }
   }
-  int total;
-  const int excl = block_excl_scan(need, sh, &total);
-  const int found = take_pages(v, total, fresh, sh);
+  int excl;
+  const int found = take_pages(v, need, free0, fresh, sh, &excl);
   if (b < s.n) {
     if (need > 0 && excl + need > found) st = STARKV_SEQ_NO_PAGES;
     pre[b] = excl;
@@ -143,7 +185,7 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan(PagedView v, Seqs<N> s
     ok[b] = st == STARKV_SEQ_OK;
     status[b] = st;
     const bool copy = ok[b] && old >= 0;
-    info[b] = i32x4{copy ? old : -1, copy ? fresh[excl] : -1, part, 0};
+    info[b] = i32x4{copy ? old : -1, copy ? fresh.at(excl) : -1, part, 0};
     if (ok[b]) v.len[s.slot[b]] = len1;
     if (copy) atomicSub(&v.refs[old], 1);
   }
@@ -151,7 +193,7 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan(PagedView v, Seqs<N> s
   for (int k = threadIdx.x; k < found; k += kPlanThreads) {
     const int o = owner_of(pre, s.n, k);
     if (!ok[o]) continue;
-    const int page = fresh[k];
+    const int page = fresh.at(k);
     table_row(v, s.slot[o])[first[o] + (k - pre[o])] = page;
     v.refs[page] = 1;
   }
@@ -245,11 +287,14 @@ __global__ __launch_bounds__(256) void free_kernel(PagedView v, Seqs<N> s, int k
 template <int N>
 __global__ __launch_bounds__(kPlanThreads) void compact_plan(PagedView v, Seqs<N> s, bool whole,
                                                              int B, const int32_t* counts,
-                                                             int tail, int32_t* fresh, i32x4* info,
+                                                             int tail, int32_t* rest, i32x4* info,
                                                              int32_t* old, int32_t* status) {
   __shared__ int pre[kMaxSeqs], first[kMaxSeqs], last[kMaxSeqs], end[kMaxSeqs];
-  __shared__ int sh[kPlanThreads / 64];
+  __shared__ int sh[kPlanThreads / 64][2];
+  __shared__ int32_t low[kLowFresh];
+  const Fresh fresh{low, rest};
   const int b = threadIdx.x;
+  const unsigned free0 = free_pages(v, b * kScan);
   int need = 0, col = 0, st = STARKV_SEQ_OK, len0 = 0, a = 0, cnt = 0, len1 = 0;
   if (b < s.n) {
     len0 = seq_len(v, s.slot[b]);
@@ -269,9 +314,8 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan(PagedView v, Seqs<N
       need = pages_of(v, to) - col;
     }
   }
-  int total;
-  const int excl = block_excl_scan(need, sh, &total);
-  const int found = take_pages(v, total, fresh, sh);
+  int excl;
+  const int found = take_pages(v, need, free0, fresh, sh, &excl);
   if (b < s.n) {
     if (need > 0 && excl + need > found) st = STARKV_SEQ_NO_PAGES;
     const bool ok = st == STARKV_SEQ_OK;
@@ -300,7 +344,7 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan(PagedView v, Seqs<N
   for (int k = threadIdx.x; k < found; k += kPlanThreads) {
     const int o = owner_of(pre, s.n, k);
     if (first[o] < 0) continue;
-    const int page = fresh[k];
+    const int page = fresh.at(k);
     table_row(v, s.slot[o])[first[o] + (k - pre[o])] = page;
     v.refs[page] = 1;
   }
