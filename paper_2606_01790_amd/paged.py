@@ -118,7 +118,9 @@ class Cache:
         self.ref = ctypes.byref(self.c)
 
     def layers(self, first: int, count: int = 1) -> "Cache":
-        """The same pages, `count` of the layers: for calls layer by layer."""
+        """The same pages, `count` of the layers, to write and attend layer by
+        layer.  (grow and compact take the whole cache: they copy rows of every
+        layer that they are given, and change the one table.)"""
         return Cache(self.k[first:first + count], self.v[first:first + count], self.table,
                      self.length, self.refs, self.H)
 
