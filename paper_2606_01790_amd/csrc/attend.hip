@@ -27,7 +27,7 @@
 // itself 41 to 45 (5.6 to 6.1 TB/s; a copy makes 4.9); one token over 13,711 in
 // 28 layers 141 us (5.6 TB/s); over 700 in one layer 11 us, the two launches and
 // their chains of loads.  float32, 4 trees of up to 13 tokens in 4 layers 39 us,
-// 8 trees of up to 48 over 1,664 to 39,197 tokens 370 (54 TFLOP/s of 154).
+// 8 trees of up to 48 over 1,664 to 39,197 tokens 405 (49 TFLOP/s of 154).
 #include <algorithm>
 
 #include "attend.h"

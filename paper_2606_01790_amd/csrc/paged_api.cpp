@@ -133,9 +133,11 @@ int split_count(const AttendShape& s, int n, int d, int esz, int64_t steps, int6
     // over 3,200 tokens (float32: 1,536), or one long sequence would hold up
     // the rest (28 layers of five sequences of 1,000 to 5,000 tokens 241 us
     // without and 234 with; float32, eight trees over 1,664 to 39,197 tokens
-    // 437 and 370)
+    // 437 and 405), as far as 4,096 blocks go: the bound on the lengths may be
+    // a whole table row, of which little is in use, and every split has its
+    // place in the workspace
     const int64_t longest = esz == 2 ? 100 : 48;
-    const int64_t even = n > 1 ? (steps + longest - 1) / longest : 1;
+    const int64_t even = n > 1 ? std::min((steps + longest - 1) / longest, 4096 / s.units) : 1;
     const int64_t ns = std::min((steps + least - 1) / least, std::max(even, blocks / s.units));
     return (int)std::max<int64_t>(1, std::min(ns, most));
   }

@@ -352,6 +352,20 @@ def test_splits_and_short_bounds():
             assert torch.equal(a, c.out) and torch.equal(l, c.lse)
 
 
+@pytest.mark.parametrize("dtype,T", [("bf16", 1), ("bf16", 9), ("bf16", 20), ("f32", 2)])
+def test_as_many_sequences_as_a_call_takes(dtype, T):
+    """256 sequences, some without rows, some without tokens; one far longer
+    than the others, so that all are split for its sake."""
+    r = np.random.default_rng(40 + T)
+    lens = r.integers(0, 40, 256).tolist()
+    lens[77] = 3500
+    rows = [int(x) for x in r.integers(0, T + 1, 256)]
+    rows[77], rows[0], rows[255] = T, 0, 0
+    c = Case(41 + T, lens, rows, 4, 2, 64, 16, dtype)
+    run("causal", c, max_len=4000)
+    run("window", c, window=3000, sinks=6, max_len=20000)
+
+
 def test_a_slot_twice_no_lse_and_no_rows():
     c = Case(17, [70, 70], [4, 4], 4, 2, 64, 16)
     c.m.table[c.slots[1]] = c.m.table[c.slots[0]]

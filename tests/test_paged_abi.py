@@ -256,6 +256,18 @@ def test_attention_of_more_rows_than_a_launch_holds():
                                        BIG, None)) == "E_PARAM"
 
 
+@pytest.mark.parametrize("dtype", [sk.BF16, sk.F32])
+@pytest.mark.parametrize("n_layers,n,rows", [(1, 32, 1), (28, 32, 1), (28, 256, 1), (1, 256, 4), (4, 8, 40),
+                                             (28, 1, 64)])
+def test_workspace_of_long_table_rows(dtype, n_layers, n, rows):
+    """At most 4,096 partial tiles of 128 rows, whatever the bound on the
+    lengths."""
+    c = cache(dtype=dtype, n_layers=n_layers, max_pages=1 << 20)
+    got = pg.lib().starkv_attend_workspace_bytes(ctypes.byref(c), ints([rows] * n), n, 1 << 26)
+    tile = 16 if dtype == sk.F32 or rows == 1 else 32 if rows == 4 else 128
+    assert 0 <= got <= 4096 * tile * (128 + 2) * 4 + 1024
+
+
 def test_the_binding_refuses_host_tensors():
     k = torch.zeros(1, 4, 2, 16, 64, dtype=torch.bfloat16)
     i = lambda *s: torch.zeros(*s, dtype=torch.int32)
