@@ -35,15 +35,17 @@ struct AttendLists {      // with PagedView and AttendArgs below 4 KB of kernel 
 };
 
 // The last b with first[b] <= k: the sequence of row tile k (sequences
-// without rows have no tile and are passed over).  The lanes of a wave
-// compare, so that there is one load to wait for.
+// without rows have no tile and are passed over).  The list lies among the
+// kernel's arguments, which vector loads fetch from memory every time: all
+// steps are uniform, so that they go through the scalar cache.
 __device__ inline int tile_owner(const int32_t* first, int n, int k) {
-  if (n == 1) return 0;
-  const int lane = threadIdx.x & 63;
-  int count = 0;
-  for (int i = 0; i < n; i += 64)
-    count += __popcll(__ballot(i + lane < n && first[min(i + lane, n - 1)] <= k));
-  return __builtin_amdgcn_readfirstlane(count) - 1;
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (first[mid] <= k) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
 }
 
 // Blocks are dealt to the 8 XCDs round-robin by number.  Work items that

@@ -23,11 +23,11 @@
 // and are bound by it from a few tiles of rows on.
 //
 // Measured, with the join: one token of each of 32 sequences of 37 to 40,941
-// tokens under a window of 4,096 and 4 sinks (252 MB) 47 to 55 us, the kernel
+// tokens under a window of 4,096 and 4 sinks (252 MB) 46 to 55 us, the kernel
 // itself 41 to 45 (5.6 to 6.1 TB/s; a copy makes 4.9); one token over 13,711 in
 // 28 layers 141 us (5.6 TB/s); over 700 in one layer 11 us, the two launches and
-// their chains of loads.  float32, 4 trees of up to 13 tokens in 4 layers 39 us,
-// 8 trees of up to 48 over 1,664 to 39,197 tokens 405 (49 TFLOP/s of 154).
+// their chains of loads.  float32, 4 trees of up to 13 tokens in 4 layers 37 us,
+// 8 trees of up to 48 over 1,664 to 39,197 tokens 355 (56 TFLOP/s of 154).
 #include <algorithm>
 
 #include "attend.h"
@@ -141,12 +141,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, quad = lane >> 4;
   // `run` tiles of one split of a (layer, group) follow each other: they read
-  // the same K and V where they are of one sequence
+  // the same K and V.  All (layer, group)s of a run are together and the
+  // splits, of which short sequences have fewer, come last, so that each XCD
+  // gets the same share of every sequence.  With the splits first it got every
+  // eighth item, of 2, 4 or 8 splits always the same (one token of five
+  // sequences of 1,000 to 5,000 tokens in 28 layers 234 us and now 167, of 64
+  // sequences in one 94 and 85)
   const unsigned item = xcd_item(blockIdx.x, run);
-  const unsigned runs = (a.n_tiles + run - 1) / run, at_run = item / run;
-  const int split = at_run % a.n_split, lg = at_run / a.n_split / runs;
-  const int tile = at_run / a.n_split % runs * run + item % run;
-  if (lg >= v.n_layers * v.G || tile >= a.n_tiles) return;
+  const unsigned lgs = v.n_layers * v.G, runs = (a.n_tiles + run - 1) / run, at_run = item / run;
+  const int lg = at_run % lgs, split = at_run / lgs / runs;
+  const int tile = at_run / lgs % runs * run + item % run;
+  if (split >= a.n_split || tile >= a.n_tiles) return;
   const int unit = lg * a.n_tiles + tile;
   const int g = lg % v.G, layer = lg / v.G;
   const int b = tile_owner(s.tile0, s.r.n, tile);
@@ -473,7 +478,7 @@ __global__ __launch_bounds__(kThreads) void attend_join(PagedView v, AttendArgs 
 template <typename T, int D>
 int launch(const PagedView& v, const AttendArgs& a, const AttendLists& l, const AttendShape& s,
            hipStream_t st) {
-  const unsigned run = (unsigned)std::min(s.n_tiles, 4);
+  const unsigned run = (unsigned)std::min(s.seq_tiles, 4);
   const unsigned runs = (s.n_tiles + run - 1) / run * v.n_layers * v.G * s.n_split;
   const unsigned blocks = (runs + 7) / 8 * 8 * run;
   if (s.many) {

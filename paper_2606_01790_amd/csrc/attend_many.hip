@@ -462,8 +462,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_many(PagedView v, Atten
 
 int launch_attend_many(const PagedView& v, const AttendArgs& a, const AttendLists& l,
                        const AttendShape& s, hipStream_t st) {
-  // the row tiles of a (layer, group) that one XCD takes at a time
-  const unsigned run = (unsigned)std::min(s.n_tiles, 4);
+  // the row tiles of a sequence that one XCD takes at a time
+  const unsigned run = (unsigned)std::min(s.seq_tiles, 4);
   const unsigned runs = (unsigned)((s.n_tiles + run - 1) / run) * v.n_layers * v.G * s.n_split;
   const unsigned blocks = (runs + 7) / 8 * 8 * run;
   if (v.d == 128) attend_many<128><<<blocks, 64 * kWaves, 0, st>>>(v, a, l, run);

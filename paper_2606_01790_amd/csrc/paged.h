@@ -74,6 +74,7 @@ struct AttendShape {
   int n_rows;       // query tokens of the call
   int row_tile;     // rows of a block
   int n_tiles;      // row tiles of one (layer, group), over all sequences
+  int seq_tiles;    // the most of one sequence
   int n_split;      // splits of the tokens
   int chunk;        // tokens that a split takes at least
   int steps;        // the most steps that a row tile walks

@@ -123,17 +123,16 @@ int split_count(const AttendShape& s, int n, int d, int esz, int64_t steps, int6
     // Measured, 256 against 512 tokens: one sequence of 13,711 tokens 13.7 and
     // 15.6 us, eight trees of four tokens (28 rows) 47.8 and 34.3
     const int64_t least = s.row_tile == 32 ? 16 : 8;
-    // and of so many blocks in all that each CU has two, which keep HBM busy;
-    // float32, bound by its matrix instructions, takes twice as many, which
-    // come out more even.  512 against 1,024 blocks: 28 layers of 4 trees of 4
-    // tokens 127 and 145 us, 64 sequences of one token 94 and 103, 12 of 3,000
-    // to 9,000 tokens 59 and 54; float32 trees of up to 13 tokens 62 and 39
-    const int64_t blocks = esz == 2 ? 512 : 1024;
+    // and of so many blocks in all that each CU has two, which keep HBM busy.
+    // 512 against 1,024 blocks: 28 layers of 4 trees of 4 tokens 126 and 148
+    // us, 64 sequences of one token 85 and 92, float32 trees of up to 13 tokens
+    // 37 and 40; 12 sequences of 3,000 to 9,000 tokens 62 and 54
+    const int64_t blocks = 512;
     // of several sequences, whose lengths may be far from each other, none of
     // over 3,200 tokens (float32: 1,536), or one long sequence would hold up
-    // the rest (28 layers of five sequences of 1,000 to 5,000 tokens 241 us
-    // without and 234 with; float32, eight trees over 1,664 to 39,197 tokens
-    // 437 and 405), as far as 4,096 blocks go: the bound on the lengths may be
+    // the rest (two layers of 18 trees of 3 tokens over 215 to 30,867 140 us
+    // without and 128 with; float32, eight trees over 1,664 to 39,197 tokens
+    // 442 and 355), as far as 4,096 blocks go: the bound on the lengths may be
     // a whole table row, of which little is in use, and every split has its
     // place in the workspace
     const int64_t longest = esz == 2 ? 100 : 48;
@@ -208,6 +207,7 @@ starkv_status attend_shape(const PagedView& v, const int32_t* rows, int n, int32
   // threads; and a sequence's rows stay below 2^31)
   if (s->units > 1 << 23) return STARKV_E_PARAM;
   s->n_tiles = (int)tiles;
+  s->seq_tiles = (int)std::max<int64_t>(1, (R + s->row_tile - 1) / s->row_tile);
   s->stat_off = s->steps_off = s->ws_bytes = 0;
   s->steps = (int)steps;
   s->balance = s->many && n > 1 && s->n_split > 1;
