@@ -8,6 +8,7 @@
  *   starkv_pages_init     an empty pool
  *   starkv_pages_grow     pages for new tokens (shared pages copied on write)
  *   starkv_pages_write    K and V of the new tokens into their pages
+ *     ..._write_grown     the same behind a grow that may have found no pages
  *   starkv_pages_fork     a sequence that shares another's pages
  *   starkv_pages_free     pages of dropped tokens back to the pool
  *   starkv_pages_compact  the kept tokens into fresh pages (a selection of
@@ -114,12 +115,23 @@ starkv_status starkv_pages_grow(const starkv_paged* cache, const int32_t* slots,
  * r of k and v, layout *rows_layout with "token" the row number over all
  * sequences of the call in order, group the KV group.  Tokens without a page,
  * of a page that another sequence shares, or before the sequence's first are
- * not written.  (After a grow that left a sequence unchanged, its last tokens
- * are older ones.)  k, v: device, the cache's dtype.
+ * not written.  After a grow that left a sequence unchanged its last tokens are
+ * older ones, and this call writes over them: behind a grow whose status the
+ * host has not read, the call below is the one.  k, v: device, the cache's
+ * dtype.
  * Errors: E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_PARAM, E_HIP. */
 starkv_status starkv_pages_write(const starkv_paged* cache, const int32_t* slots, int32_t n,
                                  const int32_t* rows, const void* k, const void* v,
                                  const starkv_kv_layout* rows_layout, void* stream);
+
+/* The same for the tokens of a grow: sequence b is written where grown[b] is
+ * STARKV_SEQ_OK, and stays as it is otherwise.  grown: device, int32 [n], the
+ * status of the starkv_pages_grow that made the tokens, of the same slots in
+ * the same order.  Errors: as above. */
+starkv_status starkv_pages_write_grown(const starkv_paged* cache, const int32_t* slots, int32_t n,
+                                       const int32_t* rows, const void* k, const void* v,
+                                       const starkv_kv_layout* rows_layout, const int32_t* grown,
+                                       void* stream);
 
 /* Make the sequence in dst[i] a fork of the one in src[i]: the same pages and
  * length, no row copied.  What dst held is freed first.  dst: no slot twice,

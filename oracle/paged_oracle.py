@@ -79,12 +79,16 @@ class PagedModel:
             status.append(OK)
         return np.array(status, dtype=np.int32)
 
-    def write(self, slots, rows, k, v):
-        """k, v: [n_layers, sum(rows), G, d]"""
+    def write(self, slots, rows, k, v, grown=None):
+        """k, v: [n_layers, sum(rows), G, d]; grown: the status of the grow
+        that made the rows"""
         r = 0
-        for b, T in zip(slots, rows):
-            for i in range(T):
-                t = int(self.len[b]) - T + i
+        for i, (b, T) in enumerate(zip(slots, rows)):
+            if grown is not None and grown[i] != OK:
+                r += T
+                continue
+            for j in range(T):
+                t = int(self.len[b]) - T + j
                 w = self.at(b, t) if t >= 0 else None
                 if w is not None and self.refs[w[0]] <= 1:
                     self.k[:, w[0], :, w[1]] = k[:, r]

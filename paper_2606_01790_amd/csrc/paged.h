@@ -39,6 +39,7 @@ struct RowList {
   int32_t n;
   int32_t slot[kMaxSeqs];
   int32_t row0[kMaxSeqs + 1];
+  const int32_t* grown = nullptr;   // device: the status of the grow that made the rows, if any
 };
 
 starkv_status check_paged(const starkv_paged* c, PagedView* v);

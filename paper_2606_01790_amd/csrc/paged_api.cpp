@@ -246,6 +246,32 @@ starkv_status attend(const starkv_paged* cache, const int32_t* slots, int32_t n,
   return hip_status(launch_attend(v, *c, stream));
 }
 
+starkv_status write(const starkv_paged* cache, const int32_t* slots, int32_t n,
+                    const int32_t* rows, const void* k, const void* vv,
+                    const starkv_kv_layout* lay, const int32_t* grown, void* stream) {
+  PagedView v;
+  starkv_status st = check_paged(cache, &v);
+  if (st != STARKV_OK) return st;
+  if ((st = check_slots(v, slots, n, true)) != STARKV_OK) return st;
+  if (n == 0) return STARKV_OK;
+  if (!rows || !lay) return STARKV_E_NULL;
+  RowList r;
+  if ((st = take_rows(v, slots, rows, n, &r)) != STARKV_OK) return st;
+  r.grown = grown;
+  if (lay->layer_stride < 0 || lay->group_stride < 0 || lay->token_stride < 0)
+    return STARKV_E_SHAPE;
+  if (r.row0[n] == 0) return STARKV_OK;
+  if (!k || !vv) return STARKV_E_NULL;
+  const int64_t e = v.esz;
+  if (lay->layer_stride > INT64_MAX / 8 || lay->group_stride > INT64_MAX / 8 ||
+      lay->token_stride > INT64_MAX / 8)
+    return STARKV_E_SHAPE;
+  if (lay->layer_stride * e % 16 || lay->group_stride * e % 16 || lay->token_stride * e % 16 ||
+      !at(k, 16) || !at(vv, 16) || !at(grown, 4))
+    return STARKV_E_ALIGN;
+  return hip_status(launch_pages_write(v, r, k, vv, *lay, stream));
+}
+
 }  // namespace
 
 }  // namespace starkv
@@ -295,28 +321,17 @@ starkv_status starkv_pages_grow(const starkv_paged* cache, const int32_t* slots,
 }
 
 starkv_status starkv_pages_write(const starkv_paged* cache, const int32_t* slots, int32_t n,
-                                 const int32_t* rows, const void* k, const void* vv,
+                                 const int32_t* rows, const void* k, const void* v,
                                  const starkv_kv_layout* lay, void* stream) {
-  PagedView v;
-  starkv_status st = check_paged(cache, &v);
-  if (st != STARKV_OK) return st;
-  if ((st = check_slots(v, slots, n, true)) != STARKV_OK) return st;
-  if (n == 0) return STARKV_OK;
-  if (!rows || !lay) return STARKV_E_NULL;
-  RowList r;
-  if ((st = take_rows(v, slots, rows, n, &r)) != STARKV_OK) return st;
-  if (lay->layer_stride < 0 || lay->group_stride < 0 || lay->token_stride < 0)
-    return STARKV_E_SHAPE;
-  if (r.row0[n] == 0) return STARKV_OK;
-  if (!k || !vv) return STARKV_E_NULL;
-  const int64_t e = v.esz;
-  if (lay->layer_stride > INT64_MAX / 8 || lay->group_stride > INT64_MAX / 8 ||
-      lay->token_stride > INT64_MAX / 8)
-    return STARKV_E_SHAPE;
-  if (lay->layer_stride * e % 16 || lay->group_stride * e % 16 || lay->token_stride * e % 16 ||
-      !at(k, 16) || !at(vv, 16))
-    return STARKV_E_ALIGN;
-  return hip_status(launch_pages_write(v, r, k, vv, *lay, stream));
+  return write(cache, slots, n, rows, k, v, lay, nullptr, stream);
+}
+
+starkv_status starkv_pages_write_grown(const starkv_paged* cache, const int32_t* slots, int32_t n,
+                                       const int32_t* rows, const void* k, const void* v,
+                                       const starkv_kv_layout* lay, const int32_t* grown,
+                                       void* stream) {
+  if (n > 0 && !grown) return STARKV_E_NULL;
+  return write(cache, slots, n, rows, k, v, lay, grown, stream);
 }
 
 starkv_status starkv_pages_fork(const starkv_paged* cache, const int32_t* src,

@@ -222,12 +222,14 @@ struct WriteArgs {
   const char* k;
   const char* v;
   int64_t ls, gs, ts;   // byte strides
+  const int32_t* grown;
 };
 
 // 16-byte vectors of K and V, one per thread (or, where a launch cannot hold
 // as many threads, several).  The page of a token must belong to its sequence
-// alone: a shared one is left as it is.  (One token of 16 sequences in 28
-// layers: 3.6 us, a chain of four loads.)
+// alone: a shared one is left as it is.  So is a sequence that the grow before
+// it left unchanged: its last tokens are not the ones to write.  (One token of
+// 16 sequences in 28 layers: 3.6 us, a chain of four loads.)
 template <int VPR, int N>
 __global__ __launch_bounds__(256) void write_kernel(PagedView v, Rows<N> r, WriteArgs a) {
   const int64_t n = (int64_t)r.row0[r.n] * v.G * VPR;
@@ -237,6 +239,7 @@ __global__ __launch_bounds__(256) void write_kernel(PagedView v, Rows<N> r, Writ
     const int64_t rg = i / VPR;
     const int g = (int)(rg % v.G), row = (int)(rg / v.G);
     const int b = owner_of(r.row0, r.n, row);
+    if (a.grown && a.grown[b] != STARKV_SEQ_OK) continue;
     const int t = seq_len(v, r.slot[b]) - r.row0[b + 1] + row;
     if (t < 0) continue;
     const int page = table_row(v, r.slot[b])[t >> v.psh];
@@ -452,7 +455,7 @@ int launch_pages_grow(const PagedView& v, const SeqList& s, const PagesWs& w, in
 int launch_pages_write(const PagedView& v, const RowList& r, const void* k, const void* vv,
                        const starkv_kv_layout& lay, void* stream) {
   WriteArgs a{static_cast<const char*>(k), static_cast<const char*>(vv), lay.layer_stride * v.esz,
-              lay.group_stride * v.esz, lay.token_stride * v.esz};
+              lay.group_stride * v.esz, lay.token_stride * v.esz, r.grown};
   const int64_t nvec = (int64_t)r.row0[r.n] * v.G * (v.d * v.esz / 16);
   const unsigned blocks = (unsigned)std::min((nvec + 255) / 256, kMaxBlocks);
   by_row_vectors(v, [&](auto vpr) {

@@ -44,6 +44,8 @@ SIGNATURES = {
                                     c_void_p]),
     "starkv_pages_write": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, _L,
                                      c_void_p]),
+    "starkv_pages_write_grown": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, _L,
+                                           c_void_p, c_void_p]),
     "starkv_pages_fork": (c_int32, [_P, c_void_p, c_void_p, c_int32, c_void_p]),
     "starkv_pages_free": (c_int32, [_P, c_void_p, c_int32, c_int32, c_int32, c_void_p]),
     "starkv_pages_compact": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_void_p, c_int64, c_int32,
@@ -215,10 +217,12 @@ def pages_grow(cache: Cache, slots, add, status, ws, stream=None):
          _bytes(ws))
 
 
-def pages_write(cache: Cache, slots, rows, k, v, layout: KVLayout, stream=None):
+def pages_write(cache: Cache, slots, rows, k, v, layout: KVLayout, stream=None, grown=None):
     """k, v: K and V of the sequences' new tokens, `layout` over (layer, group,
     row): rows_layout of a [n_layers, rows, G, d] tensor, or contiguous_layout
-    of a compacted cache's [n_layers, G, rows, d]."""
+    of a compacted cache's [n_layers, G, rows, d].  grown: the status of the
+    pages_grow of the same slots that made the tokens (starkv_pages_write_grown):
+    a sequence that it left unchanged stays so."""
     n, tot = len(slots), sum(rows)
     if len(rows) != n:
         raise ValueError("rows: one number per slot")
@@ -229,8 +233,12 @@ def pages_write(cache: Cache, slots, rows, k, v, layout: KVLayout, stream=None):
         have = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
         if tot and have < last:
             raise ValueError(f"{what}: {have} elements < {last} required")
-    _run("starkv_pages_write", cache, stream, _ints(slots), n, _ints(rows), _ptr(k), _ptr(v),
-         ctypes.byref(layout))
+    args = (_ints(slots), n, _ints(rows), _ptr(k), _ptr(v), ctypes.byref(layout))
+    if grown is None:
+        _run("starkv_pages_write", cache, stream, *args)
+    else:
+        _int32(grown, n, "grown", cache.device)
+        _run("starkv_pages_write_grown", cache, stream, *args, _ptr(grown))
 
 
 def pages_fork(cache: Cache, src, dst, stream=None):
