@@ -13,6 +13,7 @@
  *   starkv_pages_free     pages of dropped tokens back to the pool
  *   starkv_pages_compact  the kept tokens into fresh pages (a selection of
  *                         starkv_select, or the accepted path of a tree)
+ *     ..._compact_grown   the same behind a grow that may have found no pages
  *   starkv_attend_tree    attention of a tree of drafted tokens
  *   starkv_attend_window  attention with a sliding window and sink tokens
  *
@@ -171,6 +172,17 @@ starkv_status starkv_pages_compact(const starkv_paged* cache, const int32_t* slo
                                    int64_t idx_layer_stride, int32_t B, const int32_t* counts,
                                    int32_t tail, int32_t* status, void* ws, size_t ws_bytes,
                                    void* stream);
+
+/* The same for tokens that a grow made, as the drafted ones are: where grown[b]
+ * is not STARKV_SEQ_OK the last `span` tokens are older ones, which the call
+ * keeps: the sequence stays as it is, and status[b] becomes grown[b].  grown:
+ * as for starkv_pages_write_grown; it may be `status` itself. */
+starkv_status starkv_pages_compact_grown(const starkv_paged* cache, const int32_t* slots,
+                                         int32_t n, const int32_t* span, const int32_t* idx,
+                                         int64_t idx_layer_stride, int32_t B,
+                                         const int32_t* counts, int32_t tail,
+                                         const int32_t* grown, int32_t* status, void* ws,
+                                         size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------ */
 /* attention over the pages                                            */

@@ -121,13 +121,17 @@ class PagedModel:
             if keep_last == 0:
                 self.len[b] = min(n, keep_first)
 
-    def compact(self, slots, idx, tail=0, span=None, counts=None):
-        """idx: [n_layers or 1, n, B]"""
+    def compact(self, slots, idx, tail=0, span=None, counts=None, grown=None):
+        """idx: [n_layers or 1, n, B]; grown: the status of the grow that made
+        the span"""
         free, status, short = self._free_pages(), [], False
         moves = []
         k0, v0 = self.k.copy(), self.v.copy()
         for i, b in enumerate(slots):
             n = int(self.len[b])
+            if grown is not None and grown[i] != OK:
+                status.append(grown[i])
+                continue
             s = n if span is None else min(int(span[i]), n)
             a, B = n - s, idx.shape[2]
             cnt = B if counts is None else min(max(int(counts[i]), 0), B)

@@ -32,6 +32,7 @@ struct SeqList {
   int32_t n;
   int32_t slot[kMaxSeqs];
   int32_t num[kMaxSeqs];    // per sequence: tokens added, a span, or the slot forked from
+  const int32_t* grown = nullptr;   // compact, device: the status of the grow before it, if any
 };
 
 // Rows of the sequences of a call: sequence b has rows [row0[b], row0[b+1]).

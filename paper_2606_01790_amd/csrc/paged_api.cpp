@@ -272,6 +272,35 @@ starkv_status write(const starkv_paged* cache, const int32_t* slots, int32_t n,
   return hip_status(launch_pages_write(v, r, k, vv, *lay, stream));
 }
 
+starkv_status compact(const starkv_paged* cache, const int32_t* slots, int32_t n,
+                      const int32_t* span, const int32_t* idx, int64_t idx_layer_stride, int32_t B,
+                      const int32_t* counts, int32_t tail, const int32_t* grown, int32_t* status,
+                      void* ws, size_t ws_bytes, void* stream) {
+  PagedView v;
+  starkv_status st = check_paged(cache, &v);
+  if (st != STARKV_OK) return st;
+  if ((st = check_slots(v, slots, n, true)) != STARKV_OK) return st;
+  if (B < 0 || tail < 0 || (int64_t)B + tail > kMaxTokens) return STARKV_E_BUDGET;
+  if (idx_layer_stride < 0) return STARKV_E_SHAPE;
+  if (n == 0) return STARKV_OK;
+  if (!status || (B > 0 && !idx)) return STARKV_E_NULL;
+  SeqList s;
+  s.n = n;
+  s.grown = grown;
+  for (int b = 0; b < n; ++b) {
+    if (span && (span[b] < 0 || span[b] > kMaxTokens)) return STARKV_E_PARAM;
+    s.slot[b] = slots[b];
+    s.num[b] = span ? span[b] : 0;
+  }
+  if (!at(status, 4) || !at(idx, 4) || !at(counts, 4) || !at(grown, 4))
+    return STARKV_E_ALIGN;
+  const PagesWs w = pages_ws(v, n, (int64_t)B + tail);
+  if (!ws || ws_bytes < w.bytes) return STARKV_E_WORKSPACE;
+  if (!at(ws, 16)) return STARKV_E_ALIGN;
+  return hip_status(launch_pages_compact(v, s, span == nullptr, idx, idx_layer_stride, B, counts,
+                                         tail, w, status, ws, stream));
+}
+
 }  // namespace
 
 }  // namespace starkv
@@ -374,27 +403,19 @@ starkv_status starkv_pages_compact(const starkv_paged* cache, const int32_t* slo
                                    int64_t idx_layer_stride, int32_t B, const int32_t* counts,
                                    int32_t tail, int32_t* status, void* ws, size_t ws_bytes,
                                    void* stream) {
-  PagedView v;
-  starkv_status st = check_paged(cache, &v);
-  if (st != STARKV_OK) return st;
-  if ((st = check_slots(v, slots, n, true)) != STARKV_OK) return st;
-  if (B < 0 || tail < 0 || (int64_t)B + tail > kMaxTokens) return STARKV_E_BUDGET;
-  if (idx_layer_stride < 0) return STARKV_E_SHAPE;
-  if (n == 0) return STARKV_OK;
-  if (!status || (B > 0 && !idx)) return STARKV_E_NULL;
-  SeqList s;
-  s.n = n;
-  for (int b = 0; b < n; ++b) {
-    if (span && (span[b] < 0 || span[b] > kMaxTokens)) return STARKV_E_PARAM;
-    s.slot[b] = slots[b];
-    s.num[b] = span ? span[b] : 0;
-  }
-  if (!at(status, 4) || !at(idx, 4) || !at(counts, 4)) return STARKV_E_ALIGN;
-  const PagesWs w = pages_ws(v, n, (int64_t)B + tail);
-  if (!ws || ws_bytes < w.bytes) return STARKV_E_WORKSPACE;
-  if (!at(ws, 16)) return STARKV_E_ALIGN;
-  return hip_status(launch_pages_compact(v, s, span == nullptr, idx, idx_layer_stride, B, counts,
-                                         tail, w, status, ws, stream));
+  return compact(cache, slots, n, span, idx, idx_layer_stride, B, counts, tail, nullptr, status, ws,
+                 ws_bytes, stream);
+}
+
+starkv_status starkv_pages_compact_grown(const starkv_paged* cache, const int32_t* slots,
+                                         int32_t n, const int32_t* span, const int32_t* idx,
+                                         int64_t idx_layer_stride, int32_t B,
+                                         const int32_t* counts, int32_t tail,
+                                         const int32_t* grown, int32_t* status, void* ws,
+                                         size_t ws_bytes, void* stream) {
+  if (n > 0 && !grown) return STARKV_E_NULL;
+  return compact(cache, slots, n, span, idx, idx_layer_stride, B, counts, tail, grown, status, ws,
+                 ws_bytes, stream);
 }
 
 size_t starkv_attend_workspace_bytes(const starkv_paged* cache, const int32_t* rows, int32_t n,

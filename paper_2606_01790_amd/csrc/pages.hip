@@ -295,7 +295,8 @@ __global__ __launch_bounds__(256) void free_kernel(PagedView v, Seqs<N> s, int k
 template <int N>
 __global__ __launch_bounds__(kPlanThreads) void compact_plan(PagedView v, Seqs<N> s, bool whole,
                                                              int B, const int32_t* counts,
-                                                             int tail, int32_t* rest, i32x4* info,
+                                                             int tail, const int32_t* grown,
+                                                             int32_t* rest, i32x4* info,
                                                              int32_t* old, int32_t* status) {
   __shared__ int pre[kMaxSeqs], first[kMaxSeqs], last[kMaxSeqs], end[kMaxSeqs];
   __shared__ int sh[kPlanThreads / 64][2];
@@ -313,7 +314,11 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan(PagedView v, Seqs<N
     // token a's page keeps the tokens before a: not where it was dropped
     const bool gone = cnt + tail > 0 && (a & (v.P - 1)) &&
                       !is_page(v, table_row(v, s.slot[b])[a >> v.psh]);
-    if (tail > span || to > v.cap || gone) {
+    // (the grow's status before this call's own, which may be written over it)
+    if (grown) st = grown[b];
+    if (st != STARKV_SEQ_OK) {
+      // its last tokens are not those that the call is about: it stays
+    } else if (tail > span || to > v.cap || gone) {
       st = STARKV_SEQ_RANGE;
     } else {
       len1 = (int)to;
@@ -495,7 +500,7 @@ int launch_pages_compact(const PagedView& v, const SeqList& s, bool whole, const
   m.B = B;
   m.tail = tail;
   with_list(s, [&](const auto& l) {
-    compact_plan<<<1, kPlanThreads, 0, st>>>(v, l, whole, B, counts, tail,
+    compact_plan<<<1, kPlanThreads, 0, st>>>(v, l, whole, B, counts, tail, s.grown,
                                              reinterpret_cast<int32_t*>(p + w.fresh),
                                              reinterpret_cast<i32x4*>(p + w.info),
                                              reinterpret_cast<int32_t*>(p + w.old), status);

@@ -51,6 +51,9 @@ SIGNATURES = {
     "starkv_pages_compact": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_void_p, c_int64, c_int32,
                                        c_void_p, c_int32, c_void_p, c_void_p, c_size_t,
                                        c_void_p]),
+    "starkv_pages_compact_grown": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_void_p, c_int64,
+                                             c_int32, c_void_p, c_int32, c_void_p, c_void_p,
+                                             c_void_p, c_size_t, c_void_p]),
     "starkv_attend_workspace_bytes": (c_size_t, [_P, c_void_p, c_int32, c_int32]),
     "starkv_attend_tree": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32,
                                      c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
@@ -252,9 +255,10 @@ def pages_free(cache: Cache, slots, keep_first: int = 0, keep_last: int = 0, str
 
 
 def pages_compact(cache: Cache, slots, idx, status, ws, tail: int = 0, span=None, counts=None,
-                  stream=None):
+                  stream=None, grown=None):
     """idx: [n_layers, n, B] int32, or [1, n, B] where all layers keep the same
-    tokens."""
+    tokens.  grown: as for pages_write (starkv_pages_compact_grown); it may be
+    `status` itself."""
     n = len(slots)
     if idx.dim() != 3 or idx.shape[0] not in (1, cache.n_layers) or idx.shape[1] != n:
         raise ValueError(f"idx: [{cache.n_layers} or 1, {n}, B] required, got {tuple(idx.shape)}")
@@ -266,9 +270,14 @@ def pages_compact(cache: Cache, slots, idx, status, ws, tail: int = 0, span=None
         raise ValueError("span: one number per slot")
     B = idx.shape[2]
     _buffer(ws, 0, "ws", cache.device)
-    _run("starkv_pages_compact", cache, stream, _ints(slots), n,
-         _ints(span) if span is not None else None, _ptr(idx), n * B if idx.shape[0] > 1 else 0, B,
-         _ptr(counts), tail, _ptr(status), _ptr(ws), _bytes(ws))
+    args = (_ints(slots), n, _ints(span) if span is not None else None, _ptr(idx),
+            n * B if idx.shape[0] > 1 else 0, B, _ptr(counts), tail)
+    out = (_ptr(status), _ptr(ws), _bytes(ws))
+    if grown is None:
+        _run("starkv_pages_compact", cache, stream, *args, *out)
+    else:
+        _int32(grown, n, "grown", cache.device)
+        _run("starkv_pages_compact_grown", cache, stream, *args, _ptr(grown), *out)
 
 
 # ------------------------------------------------------------------ attention

@@ -56,3 +56,41 @@ def test_model_keeps_what_a_failed_grow_left():
     # without the status its last three tokens are written over
     m.write([1], [3], new[:, :3], new[:, :3])
     assert (m.k[0, m.at(1, 17)[0], 0, m.at(1, 17)[1]] == 99).all()
+
+
+@built
+def test_compact_grown_arguments():
+    L = pg.lib()
+
+    def compact(c=None, slots=(1,), span=(8,), idx=FAKE, ls=0, B=4, counts=None, tail=0, grown=FAKE,
+                status=FAKE, ws=FAKE, wb=1 << 40):
+        return name(L.starkv_pages_compact_grown(ctypes.byref(c or cache()), ints(slots), len(slots),
+                                                 ints(span), idx, ls, B, counts, tail, grown, status,
+                                                 ws, wb, None))
+
+    assert compact(grown=None) == "E_NULL"
+    assert compact(grown=FAKE + 2) == "E_ALIGN"
+    assert compact(c=cache(d=96)) == "E_SHAPE"
+    assert compact(slots=[1, 1], span=[1, 1]) == "E_PARAM" and compact(span=[-1]) == "E_PARAM"
+    assert compact(idx=None) == "E_NULL" and compact(status=None) == "E_NULL"
+    assert compact(B=-1) == "E_BUDGET" and compact(ls=-1) == "E_SHAPE"
+    assert compact(ws=None) == "E_WORKSPACE" and compact(ws=FAKE + 8) == "E_ALIGN"
+    assert L.starkv_pages_compact_grown(ctypes.byref(cache()), None, 0, None, None, 0, 0, None, 0, None,
+                                        None, None, 0, None) == 0
+
+
+def test_model_compacts_no_older_tokens():
+    m = small()
+    m.grow([1, 0], [18, 2])
+    rows = np.arange(36, dtype=np.int32).reshape(1, 18, 1, 2) + 1
+    m.write([1], [18], rows, -rows)
+    k0, row = m.k.copy(), m.table[1].copy()
+    st = m.grow([1, 0], [3, 1])
+    assert list(st) == [PO.RANGE, PO.OK]
+    idx = np.array([[[0], [0]]], dtype=np.int32)
+    assert list(m.compact([1, 0], idx, span=[3, 1], grown=st)) == [PO.RANGE, PO.NO_PAGES]
+    assert m.len[1] == 18 and np.array_equal(m.table[1], row)
+    assert np.array_equal(m.k[:, row], k0[:, row])
+    m.free([0])
+    assert list(m.compact([1], idx[:, :1], span=[3])) == [PO.OK]
+    assert m.len[1] == 16          # without the status, two older tokens are gone

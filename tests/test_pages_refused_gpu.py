@@ -108,3 +108,64 @@ def test_the_binding_refuses_a_status_of_another_kind():
                       (torch.zeros(2, dtype=torch.int32), "device tensor")):
         with pytest.raises(ValueError, match=what):
             write(bad)
+
+
+def compact_grown(b, slots, idx, grown, tail=0, span=None, counts=None, own=False):
+    """`own`: the status goes where the grow's is, as one buffer for both."""
+    say(f"compact {slots} behind {list(grown)}")
+    cd = None if counts is None else torch.tensor(counts, dtype=torch.int32, device="cuda")
+    before = b.st
+    out = before if own else b.status(len(slots))
+    pg.pages_compact(b.c, slots, torch.from_numpy(idx).cuda(), out, b.ws, tail=tail, span=span,
+                     counts=cd, grown=before)
+    want = b.m.compact(slots, idx, tail, span, counts, grown)
+    b.check("compact")
+    b.same_status("compact", want)
+    return want
+
+
+@pytest.mark.parametrize("own", [False, True])
+@pytest.mark.parametrize("dtype,d,P", [("bf16", 128, 16), ("f32", 64, 32)])
+def test_a_compaction_behind_a_grow_that_failed(dtype, d, P, own):
+    """The end of a speculative step whose draft found no pages: the tokens
+    that were there stay, in the pages where they were; the others' paths are
+    cut."""
+    b = Both(P=P, d=d, dtype=dtype, n_pages=12, max_pages=4)
+    lens = [P + 5, P - 2, 3 * P + 1, 9]
+    b.grow([0, 1, 2, 3], lens)
+    b.write([0, 1, 2, 3], lens)
+    row = b.m.table[[2, 0]].copy()
+    slots, add = [2, 1, 0, 3], [P, 6, 2 * P, 4]
+    b.grow([4], [2 * P])                  # the pool is nearly taken
+    want = b.grow(slots, add)
+    assert list(want) == [2, 0, 1, 0]
+    b.st = b.st[:4].contiguous() if own else b.st
+    st = b.st
+    write_grown(b, slots, add, st, want)
+    b.free([4])                           # pages again, for the fresh ones of the compaction
+    idx = np.array([[[0, 2, 5, 6], [0, 1, 3, 5], [1, 2, 4, 9], [3, 2, 1, 0]]], dtype=np.int32)
+    got = compact_grown(b, slots, idx, want, span=add, counts=[4, 3, 2, 4], own=own)
+    assert list(got) == [2, 0, 1, 0]
+    assert np.array_equal(b.m.table[[2, 0]], row)
+    assert list(b.m.len[:4]) == [lens[0], P - 2 + 3, lens[2], 9 + 4]
+
+
+def test_a_compaction_that_follows_a_grow_refuses_for_itself():
+    """Behind a grow that went well the call's own refusals are as ever."""
+    b = Both(n_pages=8)
+    b.grow([0, 1], [20, 40])
+    b.write([0, 1], [20, 40])
+    want = b.grow([1, 0], [2, 5])
+    idx = np.zeros((1, 2, 1), dtype=np.int32)
+    assert list(compact_grown(b, [1, 0], idx, want, tail=3, span=[2, 5])) == [2, 0]
+
+
+def test_the_binding_refuses_a_compaction_with_a_status_of_another_kind():
+    b = Both()
+    b.grow([0, 1], [3, 3])
+    idx = torch.zeros(1, 2, 1, dtype=torch.int32, device="cuda")
+    for bad, what in ((torch.zeros(2, dtype=torch.int64, device="cuda"), "grown: torch.int64"),
+                      (torch.zeros(1, dtype=torch.int32, device="cuda"), "grown: 2"),
+                      (torch.zeros(2, dtype=torch.int32), "device tensor")):
+        with pytest.raises(ValueError, match=what):
+            pg.pages_compact(b.c, [0, 1], idx, b.st, b.ws, span=[1, 1], grown=bad)
