@@ -81,8 +81,8 @@ typedef struct starkv_paged {
 /* What grow and compact report per sequence of the call (int32, device). */
 #define STARKV_SEQ_OK 0
 #define STARKV_SEQ_NO_PAGES 1  /* the pool had too few free pages: unchanged */
-#define STARKV_SEQ_RANGE 2     /* past the table row, tail past the sequence, or it would go on
-                                  within a page that was dropped: unchanged */
+#define STARKV_SEQ_RANGE 2     /* past the table row, tail past the sequence or of dropped tokens,
+                                  or it would go on within a page that was dropped: unchanged */
 
 /* ------------------------------------------------------------------ */
 /* pages                                                               */
@@ -159,7 +159,8 @@ starkv_status starkv_pages_free(const starkv_paged* cache, const int32_t* slots,
  * speculative step.  The kept rows go to fresh pages (bit copies, from the
  * page of token a on); the pages that they came from are let go, and are free
  * afterwards unless other sequences share them.  Rows may be picked in any
- * order and more than once.
+ * order and more than once.  A tail of which a token was dropped has no rows to
+ * keep: STARKV_SEQ_RANGE.
  * idx:    device, int32 [n][B] per layer, layer l at idx + l*idx_layer_stride
  *         (0: all layers keep the same tokens).  An entry outside [0, span -
  *         tail), or whose token was dropped, gives an all-zero row.

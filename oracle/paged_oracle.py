@@ -137,7 +137,8 @@ class PagedModel:
             cnt = B if counts is None else min(max(int(counts[i]), 0), B)
             new = a + cnt + tail
             gone = cnt + tail > 0 and a % self.P and not self.is_page(self.table[b, a // self.P])
-            if tail > s or new > self.cap or gone:
+            lost = tail <= s and any(self.at(b, t) is None for t in range(n - tail, n))
+            if tail > s or new > self.cap or gone or lost:
                 status.append(RANGE)
                 continue
             col = a // self.P if cnt + tail else self.pages(a)

@@ -298,12 +298,27 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan(PagedView v, Seqs<N
                                                              int tail, const int32_t* grown,
                                                              int32_t* rest, i32x4* info,
                                                              int32_t* old, int32_t* status) {
-  __shared__ int pre[kMaxSeqs], first[kMaxSeqs], last[kMaxSeqs], end[kMaxSeqs];
+  __shared__ int pre[kMaxSeqs], first[kMaxSeqs], last[kMaxSeqs], end[kMaxSeqs], lost[kMaxSeqs];
   __shared__ int sh[kPlanThreads / 64][2];
   __shared__ int32_t low[kLowFresh];
   const Fresh fresh{low, rest};
-  const int b = threadIdx.x;
+  const int b = threadIdx.x, lane = threadIdx.x & 63;
   const unsigned free0 = free_pages(v, b * kScan);
+  // Tails of a few pages are looked at by the sequence's thread, beside its
+  // other table entry; longer ones by a wave, 64 pages at a time.
+  const bool few = tail <= 3 * v.P;
+  if (!few) {
+    for (int o = threadIdx.x >> 6; o < s.n; o += kPlanThreads / 64) {
+      const int n = seq_len(v, s.slot[o]);
+      const int32_t* row = table_row(v, s.slot[o]);
+      bool gone = false;
+      if (tail <= n)
+        for (int j = ((n - tail) >> v.psh) + lane; j < pages_of(v, n); j += 64) gone |= !is_page(v, row[j]);
+      gone = __any(gone);
+      if (lane == 0) lost[o] = gone;
+    }
+    __syncthreads();
+  }
   int need = 0, col = 0, st = STARKV_SEQ_OK, len0 = 0, a = 0, cnt = 0, len1 = 0;
   if (b < s.n) {
     len0 = seq_len(v, s.slot[b]);
@@ -312,8 +327,18 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan(PagedView v, Seqs<N
     cnt = counts ? min(max(counts[b], 0), B) : B;
     const int64_t to = (int64_t)a + cnt + tail;
     // token a's page keeps the tokens before a: not where it was dropped
-    const bool gone = cnt + tail > 0 && (a & (v.P - 1)) &&
-                      !is_page(v, table_row(v, s.slot[b])[a >> v.psh]);
+    bool gone = cnt + tail > 0 && (a & (v.P - 1)) &&
+                !is_page(v, table_row(v, s.slot[b])[a >> v.psh]);
+    // and a dropped token of the tail has no row: a row of zeros in its place
+    // would be seen by the attentions, which did not see the token
+    if (!few) {
+      gone |= lost[b] != 0;
+    } else if (tail > 0 && tail <= len0) {
+      const int j0 = (len0 - tail) >> v.psh, j1 = (len0 - 1) >> v.psh;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)      // tails of at most 3 P tokens end within four pages
+        if (j0 + j <= j1) gone |= !is_page(v, table_row(v, s.slot[b])[j0 + j]);
+    }
     // (the grow's status before this call's own, which may be written over it)
     if (grown) st = grown[b];
     if (st != STARKV_SEQ_OK) {
@@ -342,7 +367,6 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan(PagedView v, Seqs<N
   }
   __syncthreads();
   // a wave per sequence: the old entries kept aside and let go
-  const int lane = threadIdx.x & 63;
   for (int o = threadIdx.x >> 6; o < s.n; o += kPlanThreads / 64) {
     if (first[o] < 0) continue;
     int32_t* row = table_row(v, s.slot[o]);

@@ -94,3 +94,13 @@ def test_model_compacts_no_older_tokens():
     m.free([0])
     assert list(m.compact([1], idx[:, :1], span=[3])) == [PO.OK]
     assert m.len[1] == 16          # without the status, two older tokens are gone
+
+
+def test_model_keeps_no_dropped_tail():
+    m = small(12)
+    m.grow([0], [18])
+    m.free([0], 1, 5)                # page 0 and the last two
+    assert list(m.table[0] >= 0) == [True, False, False, True, True]
+    idx = np.zeros((1, 1, 0), dtype=np.int32)
+    assert list(m.compact([0], idx, tail=7)) == [PO.RANGE] and m.len[0] == 18
+    assert list(m.compact([0], idx, tail=6)) == [PO.OK] and m.len[0] == 6
