@@ -395,6 +395,7 @@ starkv_status starkv_pages_free(const starkv_paged* cache, const int32_t* slots,
   SeqList s;
   s.n = n;
   std::copy(slots, slots + n, s.slot);
+  std::fill(s.num, s.num + n, 0);
   return hip_status(launch_pages_free(v, s, keep_first, keep_last, stream));
 }
 
