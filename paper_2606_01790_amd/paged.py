@@ -126,10 +126,10 @@ class Cache:
         """The same pages, `count` of the layers, to write and attend layer by
         layer.  (grow and compact take the whole cache: they copy rows of every
         layer that they are given, and change the one table.)"""
-        k, v = self.k[first:first + count], self.v[first:first + count]
+        k = self.k[first:first + count]
         if count < 1 or k.shape[0] != count:     # a slice of fewer would pass for the whole
             raise ValueError(f"layers [{first}, {first + count}) of {self.n_layers}")
-        return Cache(k, v, self.table, self.length, self.refs, self.H)
+        return Cache(k, self.v[first:first + count], self.table, self.length, self.refs, self.H)
 
 
 def new_cache(n_layers: int, n_pages: int, page_tokens: int, G: int, d: int, n_slots: int,
