@@ -197,7 +197,8 @@ starkv_status starkv_pages_compact_grown(const starkv_paged* cache, const int32_
  *   x[h,t] = q[h] . K[g(h),t] / sqrt(d),
  *   out[h] = sum_{t in V(i)} softmax_t(x[h,t]) V[g(h),t],
  *   lse[h] = ln sum_{t in V(i)} exp(x[h,t]).
- * A row that sees nothing gets out = 0 and lse = -infinity.  Tokens outside
+ * A row that sees nothing gets out = 0 and lse = -infinity, and so does one
+ * whose logits are all -infinity (from K or q themselves).  Tokens outside
  * V(i), and dropped ones, do not touch row i, whatever their K and V hold
  * (infinities and NaN included).  Softmax, sums and lse are float32 (bf16
  * caches: the weights are rounded to bf16 for the product with V).
@@ -212,7 +213,9 @@ starkv_status starkv_pages_compact_grown(const starkv_paged* cache, const int32_
  * Errors: E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_PARAM, E_WORKSPACE, E_HIP. */
 
 /* Bytes of device workspace of an attention call with these arguments.  0 if
- * they are invalid, or none is needed (ws may then be NULL). */
+ * they are invalid, or none is needed (ws may then be NULL).  Calls of fewer
+ * rows, or on fewer layers, are split further and may need more: a workspace
+ * for several kinds of calls has the size of the one that needs most. */
 size_t starkv_attend_workspace_bytes(const starkv_paged* cache, const int32_t* rows, int32_t n,
                                      int32_t max_len);
 
