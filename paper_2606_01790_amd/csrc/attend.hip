@@ -25,9 +25,12 @@
 // Measured, with the join: one token of each of 32 sequences of 37 to 40,941
 // tokens under a window of 4,096 and 4 sinks (252 MB) 46 to 55 us, the kernel
 // itself 41 to 45 (5.6 to 6.1 TB/s; a copy makes 4.9); one token over 13,711 in
-// 28 layers 141 us (5.6 TB/s); over 700 in one layer 11 us, the two launches and
-// their chains of loads.  float32, 4 trees of up to 13 tokens in 4 layers 37 us,
-// 8 trees of up to 48 over 1,664 to 39,197 tokens 355 (56 TFLOP/s of 154).
+// 28 layers 142 us (5.5 TB/s), a tree of four 150; over 700 in one layer 11 us,
+// the two launches and their chains of loads.  float32: one token over 13,711 in
+// 28 layers 271 us (5.8 TB/s), one of each of 16 sequences of 3,000 to 12,000 116
+// (4.2); 4 trees of up to 13 tokens in 4 layers 35, 8 trees of up to 48 over
+// 1,664 to 39,197 tokens 347 (57 TFLOP/s of 154); a chunk of 1,000 tokens behind
+// 12,711 2,502 (76).
 #include <algorithm>
 
 #include "attend.h"

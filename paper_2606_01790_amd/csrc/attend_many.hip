@@ -17,13 +17,16 @@
 // then the weights, up to 2^8, lose nothing, and the output need not be
 // rescaled.
 //
-// Measured: the prefill of 8,192 tokens under a window of 4,096 388 us, 930
-// TFLOP/s; 2,755 tokens appended to 10,956 under a window of 8,192 392 us, 850;
-// a tree of 64 tokens over 40,941 in 28 layers 1,266 us, 830 (448 rows that
-// take the place of 512, and 54 us of joining).  A library product of 8192^3
-// makes 1,203.  The matrix units are busy in 43% of the SIMDs' cycles, LDS has
-// no bank conflicts, and the same calls on zeros run 12 to 19% faster: power,
-// and what a wave issues beside its products, hold the rest.  Short calls are
+// Measured, over several cards: the prefill of 8,192 tokens under a window of
+// 4,096 388 to 417 us, 870 to 930 TFLOP/s; 2,755 tokens appended to 10,956 under
+// a window of 8,192 392 to 400 us, 835 to 850 (25 of them the join); a tree of 64
+// tokens over 40,941 in 28 layers 1,266 to 1,306 us, 805 to 830 (448 rows that
+// take the place of 512, and 53 us of joining).  A library product of 8192^3
+// makes 1,203 to 1,370.  The matrix units are busy in 41 to 43% of the SIMDs'
+// cycles, in the library's product in 69%, at 1.9 to 2.1 GHz in both: both lose
+// by power (on zeros these calls run 12 to 19% faster), and what lies between
+// them is what a wave issues beside its products, five to six vector
+// instructions to each against one.  LDS has no bank conflicts.  Short calls are
 // bound by their chain of loads (eight tokens over 600: 9 us, and 3 to join).
 #include <algorithm>
 
