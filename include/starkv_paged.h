@@ -52,12 +52,11 @@ extern "C" {
  *   token_stride >= d and under 2^28 bytes; k and v 16-byte aligned, the int32 arrays 4-byte.
  * refs[p] is how many table entries name page p; a page is free when refs[p]
  * is 0.  Calls that allocate take the lowest-numbered pages that were free
- * when the call began, in the order of the call's sequences.  (They look for
- * them from page 0 up: 4 us for every 8,192 pages before the last that they
- * take.)  To write or
- * attend to one layer of a cache, pass n_layers = 1 and k, v moved on by the
- * layer's offset; grow and compact move rows of the layers that they are given
- * and change the table once, so they take all layers. */
+ * when the call began, in the order of the call's sequences; they look for
+ * them from page 0 up, 4 us for every 8,192 pages before the last that they
+ * take.  To write or attend to one layer of a cache, pass n_layers = 1 and k, v
+ * moved on by the layer's offset; grow and compact move rows of the layers that
+ * they are given and change the table once, so they take all layers. */
 typedef struct starkv_paged {
   int32_t n_layers;
   int32_t H;
@@ -179,7 +178,7 @@ starkv_status starkv_pages_compact(const starkv_paged* cache, const int32_t* slo
 /* The same for tokens that a grow made, as the drafted ones are: where grown[b]
  * is not STARKV_SEQ_OK the last `span` tokens are older ones, which the call
  * keeps: the sequence stays as it is, and status[b] becomes grown[b].  grown:
- * as for starkv_pages_write_grown; it may be `status` itself. */
+ * as for starkv_pages_write_grown; it may be `status` itself.  Errors: as above. */
 starkv_status starkv_pages_compact_grown(const starkv_paged* cache, const int32_t* slots,
                                          int32_t n, const int32_t* span, const int32_t* idx,
                                          int64_t idx_layer_stride, int32_t B,
