@@ -9,6 +9,7 @@
  *   starkv_pages_grow     pages for new tokens (shared pages copied on write)
  *   starkv_pages_write    K and V of the new tokens into their pages
  *     ..._write_grown     the same behind a grow that may have found no pages
+ *   starkv_pages_read     K and V of a sequence's last tokens out of their pages
  *   starkv_pages_fork     a sequence that shares another's pages
  *   starkv_pages_free     pages of dropped tokens back to the pool
  *   starkv_pages_compact  the kept tokens into fresh pages (a selection of
@@ -16,6 +17,9 @@
  *     ..._compact_grown   the same behind a grow that may have found no pages
  *   starkv_attend_tree    attention of a tree of drafted tokens
  *   starkv_attend_window  attention with a sliding window and sink tokens
+ *   starkv_mass_add       attention weights added up per cached token
+ *   starkv_mass_fork      a fork's copy of them
+ *   starkv_pages_evict    the tokens of the least accumulated weight evicted
  *
  * The conventions of starkv.h hold: asynchronous on `stream`, no allocation,
  * no copy to the host, arguments validated on the host before any GPU work
@@ -38,6 +42,21 @@ extern "C" {
 #define STARKV_MAX_SEQS 256        /* sequences per call */
 #define STARKV_MAX_DRAFT_WORDS 4   /* 64-bit mask words per drafted token */
 
+/* A cache held in 4 bits, a dtype of starkv_paged alone: 32 elements of a K or
+ * V row share a power of two.  An element is 4 bits, e2m1: a sign (bit 3) and
+ * one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (bits 0 to 2); element 2i lies in the low half
+ * of byte i.  Scale byte b stands for 2^(b - 127); 255 makes its block NaN.  A
+ * (layer, page, group)'s page_tokens rows of d/2 bytes lie one behind the other,
+ * token_stride = d/2, and behind them, from byte page_tokens*d/2 on, their
+ * scales, d/32 bytes a row: page_tokens*(d/2 + d/32) bytes in all.  Strides count
+ * bytes.  q, out, and the rows given and read are bf16.
+ *   starkv_pages_write quantises: with a the largest magnitude of 32 elements,
+ * the scale is the 2^e for which a is in (3.5, 7] * 2^e (b clamped to [2, 252]), and
+ * an element becomes the nearest of the above times 2^e, ties to the even code,
+ * beyond 6 to 6.  A block that holds an infinity or NaN becomes NaN.  Every other
+ * block stands for finite bf16 numbers, and the attentions are those over them. */
+#define STARKV_FP4 4
+
 /* A paged cache.  Token t of the sequence in slot b lies in page
  * table[b][t / page_tokens], row t % page_tokens; element (layer, page,
  * group, row, j) of K (and of V) at base + layer*layer_stride +
@@ -45,11 +64,11 @@ extern "C" {
  * entry that is not in [0, n_pages) (normally -1) is no page: its tokens are
  * dropped, and no call reads or writes memory for them.
  *   n_layers in [1, 4096], G in [1, STARKV_MAX_GROUPS], H % G == 0, H <= 4096,
- *   d in {64, 128}, dtype STARKV_F32 or STARKV_BF16,
+ *   d in {64, 128}, dtype STARKV_F32, STARKV_BF16 or STARKV_FP4,
  *   page_tokens a power of two in [16, 1024], n_pages in [1, 2^26],
  *   n_slots in [1, 2^20], max_pages*page_tokens <= 2^26,
  *   strides times the element size multiples of 16 bytes, not negative,
- *   token_stride >= d and under 2^28 bytes; k and v 16-byte aligned, the int32 arrays 4-byte.
+ *   token_stride >= d (STARKV_FP4: d/2) and under 2^28 bytes; k and v 16-byte aligned, the int32 arrays 4-byte.
  * refs[p] is how many table entries name page p; a page is free when refs[p]
  * is 0.  Calls that allocate take the lowest-numbered pages that were free
  * when the call began, in the order of the call's sequences; they look for
@@ -84,6 +103,7 @@ typedef struct starkv_paged {
 #define STARKV_SEQ_NO_PAGES 1  /* the pool had too few free pages: unchanged */
 #define STARKV_SEQ_RANGE 2     /* past the table row, tail past the sequence or of dropped tokens,
                                   or it would go on within a page that was dropped: unchanged */
+#define STARKV_SEQ_SHORT 3     /* evict: no longer than what is kept: unchanged */
 
 /* ------------------------------------------------------------------ */
 /* pages                                                               */
@@ -120,7 +140,7 @@ starkv_status starkv_pages_grow(const starkv_paged* cache, const int32_t* slots,
  * not written.  After a grow that left a sequence unchanged its last tokens are
  * older ones, and this call writes over them: behind a grow whose status the
  * host has not read, the call below is the one.  k, v: device, the cache's
- * dtype.
+ * dtype (STARKV_FP4: bf16).
  * Errors: E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_PARAM, E_HIP. */
 starkv_status starkv_pages_write(const starkv_paged* cache, const int32_t* slots, int32_t n,
                                  const int32_t* rows, const void* k, const void* v,
@@ -134,6 +154,15 @@ starkv_status starkv_pages_write_grown(const starkv_paged* cache, const int32_t*
                                        const int32_t* rows, const void* k, const void* v,
                                        const starkv_kv_layout* rows_layout, const int32_t* grown,
                                        void* stream);
+
+/* Read K and V of the last rows[b] >= 0 tokens (host) of each sequence into k
+ * and v (device out, dtype and layout as for starkv_pages_write; a slot may
+ * repeat).  A token without a page, or before the sequence's first, gives an
+ * all-zero row.  STARKV_FP4: the bf16 numbers that the rows stand for.
+ * Errors: E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_PARAM, E_HIP. */
+starkv_status starkv_pages_read(const starkv_paged* cache, const int32_t* slots, int32_t n,
+                                const int32_t* rows, void* k, void* v,
+                                const starkv_kv_layout* rows_layout, void* stream);
 
 /* Make the sequence in dst[i] a fork of the one in src[i]: the same pages and
  * length, no row copied.  What dst held is freed first.  dst: no slot twice,
@@ -201,9 +230,9 @@ starkv_status starkv_pages_compact_grown(const starkv_paged* cache, const int32_
  * A row that sees nothing gets out = 0 and lse = -infinity, and so does one
  * whose logits are all -infinity (from K or q themselves).  Tokens outside
  * V(i), and dropped ones, do not touch row i, whatever their K and V hold
- * (infinities and NaN included).  Softmax, sums and lse are float32 (bf16
- * caches: the weights are rounded to bf16 for the product with V).
- * q:   device, the cache's dtype, [n_layers][sum rows][H][d] contiguous, rows
+ * (infinities and NaN included).  Softmax, sums and lse are float32 (bf16 and
+ * 4-bit caches: the weights are rounded to bf16 for the product with V).
+ * q:   device, the cache's dtype (STARKV_FP4: bf16), [n_layers][sum rows][H][d] contiguous, rows
  *      of the call's sequences in order; 16-byte aligned.
  * out: device out, as q.   lse: device out, float32 [n_layers][sum rows][H],
  *      or NULL.
@@ -238,6 +267,70 @@ starkv_status starkv_attend_window(const starkv_paged* cache, const int32_t* slo
                                    const int32_t* rows, const void* q, int32_t window,
                                    int32_t sinks, int32_t max_len, void* out, float* lse,
                                    void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------ */
+/* eviction by accumulated attention weight                            */
+/* ------------------------------------------------------------------ */
+/* A mass is what the attention has weighted a cached token with, summed over
+ * the query tokens and heads of a layer: float32 [n_layers][n_slots][max_pages *
+ * page_tokens], device, contiguous, beside the cache.  starkv_mass_add follows
+ * each attention, starkv_mass_fork each fork, and starkv_pages_evict takes the
+ * lightest tokens away, their masses with them. */
+
+/* Add the weights of the last rows[b] >= 0 tokens (host) of each sequence: with
+ * x, window, sinks and the tokens V(i) that query token i sees as for
+ * starkv_attend_window, and lse what that call gave for these rows,
+ *   out[t] = old[t] + sum_{i, h: t in V(i)} exp(x[h,t] - lse[i,h]),
+ * old[t] = mass[t] for the tokens before the rows', 0 for the rows' own.  A row
+ * whose lse is -infinity adds nothing.  All tokens of the sequence are written
+ * (dropped ones keep old[t]), none behind it; sequences without rows are left as
+ * they are.  Logits, weights and sums are float32.
+ * slots: no slot twice (E_PARAM).   rows: each at most what a table row holds,
+ *      their sum at most 2^26 (E_PARAM).
+ * q:   as for the attentions.   lse: device, float32 [n_layers][sum rows][H].
+ * mass: device, as above.   out: device out, as mass; it may be mass.
+ * max_len, ws: as for the attentions, with starkv_mass_workspace_bytes().
+ * Errors: E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_PARAM, E_WORKSPACE, E_HIP. */
+starkv_status starkv_mass_add(const starkv_paged* cache, const int32_t* slots, int32_t n,
+                              const int32_t* rows, const void* q, const float* lse,
+                              int32_t window, int32_t sinks, int32_t max_len, const float* mass,
+                              float* out, void* ws, size_t ws_bytes, void* stream);
+
+/* Bytes of device workspace of starkv_mass_add with these arguments.  0 if they
+ * are invalid, or none is needed (ws may then be NULL). */
+size_t starkv_mass_workspace_bytes(const starkv_paged* cache, const int32_t* rows, int32_t n,
+                                   int32_t max_len);
+
+/* Copy the masses of the sequences in src to dst, after (or before)
+ * starkv_pages_fork of the same slots: the first length(src) of each.
+ * Errors: as for starkv_pages_fork. */
+starkv_status starkv_mass_fork(const starkv_paged* cache, const int32_t* src, const int32_t* dst,
+                               int32_t n, float* mass, void* stream);
+
+/* Cut each sequence longer than sinks + keep + recent down to its first `sinks`
+ * tokens, its last `recent` ones, and of those between the `keep` of the largest
+ * mass, by layer, in their order (equal masses: the lower token; NaN counts as
+ * the largest).  Dropped tokens are not kept; where that leaves fewer than asked
+ * for, the sequence ends up shorter.  Rows move as with starkv_pages_compact and
+ * tail = recent, and the masses with them.  Other sequences stay as they are,
+ * STARKV_SEQ_SHORT.
+ * slots: no slot twice (E_PARAM).   mass: device, in and out.
+ * idx:    device out, int32 [n_layers][n][sinks + keep]: the kept tokens but for
+ *         the recent ones, ascending; -1 behind the last, and for short sequences.
+ * status: device out, int32 [n] (STARKV_SEQ_*): where it is not STARKV_SEQ_OK the
+ *         sequence and its masses are as before.
+ * ws: device workspace of ws_bytes >= starkv_evict_workspace_bytes().
+ * Errors: E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_BUDGET (keep, sinks or recent
+ * negative, or their sum over 2^26), E_PARAM, E_WORKSPACE, E_HIP. */
+starkv_status starkv_pages_evict(const starkv_paged* cache, const int32_t* slots, int32_t n,
+                                 float* mass, int32_t keep, int32_t sinks, int32_t recent,
+                                 int32_t* idx, int32_t* status, void* ws, size_t ws_bytes,
+                                 void* stream);
+
+/* Bytes of device workspace that starkv_pages_evict needs for n sequences.  0 if
+ * the arguments are invalid. */
+size_t starkv_evict_workspace_bytes(const starkv_paged* cache, int32_t n, int32_t keep,
+                                    int32_t sinks, int32_t recent);
 
 #ifdef __cplusplus
 }

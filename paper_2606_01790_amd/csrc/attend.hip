@@ -32,6 +32,7 @@
 // 1,664 to 39,197 tokens 347 (57 TFLOP/s of 154); a chunk of 1,000 tokens behind
 // 12,711 2,502 (76).
 #include <algorithm>
+#include <type_traits>
 
 #include "attend.h"
 
@@ -88,6 +89,26 @@ struct VRow<float, 64> {
   static constexpr int kLoads = 1, kCols = 4;
 };
 
+// What a lane loads of a 4-bit step: the row of K of each 16-token half that it
+// holds for the products and that row's scale, and its columns of eight rows of
+// V and of four rows' scales at a time.
+template <int D>
+struct Fp4Step {
+  using KRow = std::conditional_t<D == 128, i32x4, uint2>;      // D/4 elements
+  using VRow = std::conditional_t<D == 128, uint32_t, uint16_t>;  // D/16 elements
+  using Scales = std::conditional_t<D == 128, i32x4, uint2>;    // four rows of D/32 bytes
+  KRow k[2];
+  uint8_t ks[2];
+  VRow v[8];
+  Scales vs[2];
+};
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+// Elements 2i and 2i + 1 of w, times 2^(byte - 127) (NaN for 255), exactly.
+template <int I>
+__device__ inline uint32_t from_fp4(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, I));
+}
+
 __device__ inline float max4(f32x4 v) { return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])); }
 
 __device__ inline uint32_t bf16_pair(float lo, float hi) {
@@ -126,7 +147,13 @@ __device__ inline void zero_not_finite(R& r) {
 // Two blocks to a CU at least: the registers then all come from one file, none
 // is copied, and two or three blocks fit where one or two did (eight trees of
 // four tokens 33.2 -> 27.5 us, four layers of 22 sequences 105 -> 86).
-template <typename T, int D, int NB>
+//
+// F4: a cache of 4 bits.  Its elements become bf16, exactly, by the hardware's
+// conversion, two at a time, as the fragments are made, and all else is the
+// same.  K's products may take the elements of a row in any order that Q's take
+// too: lane quad holds the D/4 neighbouring ones that it reads at once, which are
+// of one scale.
+template <typename T, int D, int NB, bool F4 = false>
 __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArgs a, AttendLists s,
                                                        unsigned run) {
   using F = Frag<T>;
@@ -175,9 +202,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
   for (int nb = 0; nb < NB; ++nb) {
     const int r = min(r0 + 16 * nb + l16, rows - 1);
     qi[nb] = r / hpg;
-    const char* qr = qbase + ((size_t)qi[nb] * v.H + g * hpg + r % hpg) * D * sizeof(T) + 16 * quad;
+    const char* qr = qbase + ((size_t)qi[nb] * v.H + g * hpg + r % hpg) * D * sizeof(T) +
+                     (F4 ? D / 2 : 16) * quad;
 #pragma unroll
-    for (int f = 0; f < NF; ++f) qf[nb][f] = *reinterpret_cast<const frag*>(qr + 64 * f);
+    for (int f = 0; f < NF; ++f) qf[nb][f] = *reinterpret_cast<const frag*>(qr + (F4 ? 16 : 64) * f);
   }
 
   float m[NB], l[NB];        // maximum; this lane's part of the sum
@@ -203,11 +231,40 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
     next0 = page_of(u, 0);
     next1 = page_of(u, 1);
   }
+  // 4 bits: a step's rows are read while the step before is worked on
+  [[maybe_unused]] Fp4Step<D> ahead;
+  [[maybe_unused]] const auto fetch = [&](int w, int p0, int p1) {
+    const int at0 = step_token<kStep>(ts, min(w, ts.nt - 1));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      using S = Fp4Step<D>;
+      const int page = h ? p1 : p0, in_page = (at0 + 16 * h) & (v.P - 1);
+      const int64_t at = base + (int64_t)(page >= 0 && page < v.n_pages ? page : 0) * v.ps;
+      const char* kr = v.k + at + in_page * (D / 2);
+      const char* vr = v.v + at + in_page * (D / 2);
+      const int scales = v.P * (D / 2) - in_page * (D / 2 - D / 32);   // from kr and vr on
+      ahead.k[h] = *reinterpret_cast<const typename S::KRow*>(kr + l16 * (D / 2) + quad * (D / 8));
+      ahead.ks[h] = *reinterpret_cast<const uint8_t*>(kr + scales + l16 * (D / 32) + quad * (D / 4) / 32);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        ahead.v[4 * h + j] = *reinterpret_cast<const typename S::VRow*>(
+            vr + (4 * quad + j) * (D / 2) + l16 * (D / 32));
+      ahead.vs[h] = *reinterpret_cast<const typename S::Scales*>(vr + scales + 4 * quad * (D / 32));
+    }
+  };
+  int page0 = next0, page1 = next1;     // 4 bits: this step's pages
+  if constexpr (F4) {
+    if (u < u1) {
+      fetch(u, next0, next1);
+      next0 = page_of(u + kWaves, 0);
+      next1 = page_of(u + kWaves, 1);
+    }
+  }
   for (; u < u1; u += kWaves) {
     const int t0 = step_token<kStep>(ts, u);
     // where there is no page the loads go to page 0 and the tokens are masked
     // below
-    int page[2] = {next0, next1};
+    int page[2] = {F4 ? page0 : next0, F4 ? page1 : next1};
     bool there[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -216,6 +273,39 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
     }
     frag kf[2][NF];
     vrow vv[8][VR::kLoads];
+    if constexpr (F4) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float ks = __uint_as_float((uint32_t)ahead.ks[h] << 23);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          const uint32_t w = reinterpret_cast<const uint32_t(&)[NF]>(ahead.k[h])[f];
+          typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+          kf[h][f] = __builtin_bit_cast(frag, u32x4{from_fp4<0>(w, ks), from_fp4<1>(w, ks),
+                                                    from_fp4<2>(w, ks), from_fp4<3>(w, ks)});
+        }
+        // the byte of the lane's columns among each row's scales
+        constexpr int kPer = D / 32;
+        const int byte = l16 * kPer / 16;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t sw = reinterpret_cast<const uint32_t(&)[kPer]>(ahead.vs[h])[j * kPer / 4];
+          const float vs = __uint_as_float((sw >> (8 * byte + j * kPer % 4 * 8) & 0xFFu) << 23);
+          const uint32_t w = ahead.v[4 * h + j];
+          vv[4 * h + j][0][0] = from_fp4<0>(w, vs);
+          vv[4 * h + j][0][1] = from_fp4<1>(w, vs);
+          if constexpr (D == 128) {
+            vv[4 * h + j][0][2] = from_fp4<2>(w, vs);
+            vv[4 * h + j][0][3] = from_fp4<3>(w, vs);
+          }
+        }
+      }
+      page0 = next0;
+      page1 = next1;
+      if (u + kWaves < u1) fetch(u + kWaves, page0, page1);
+      next0 = page_of(u + 2 * kWaves, 0);
+      next1 = page_of(u + 2 * kWaves, 1);
+    } else {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int in_page = (t0 + 16 * h) & (v.P - 1);
@@ -232,6 +322,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
     }
     next0 = page_of(u + kWaves, 0);
     next1 = page_of(u + kWaves, 1);
+    }
     const bool whole = there[0] && there[1] && sees_step<kStep>(all, t0);
 
     f32x4 x[NB][2];
@@ -305,14 +396,20 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
           }
           const int t = t0 + k;
           if (!(seen[nb] >> k & 1)) continue;
-          const char* vr = v.v + base + (int64_t)page[h] * v.ps + (int64_t)(t & (v.P - 1)) * v.ts;
+          const char* block = v.v + base + (int64_t)page[h] * v.ps;
+          const char* vr = block + (int64_t)(t & (v.P - 1)) * v.ts;
 #pragma unroll
           for (int e = 0; e < ND; ++e)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int col = 16 * VR::kCols * (e / VR::kCols) + VR::kCols * (4 * quad + i) +
                               e % VR::kCols;
-              const float val = (float)reinterpret_cast<const T*>(vr)[col];
+              float val;
+              if constexpr (F4)      // a block of 4 bits is NaN or finite as a whole
+                val = (uint8_t)block[v.P * (D / 2) + (t & (v.P - 1)) * (D / 32) + col / 32] == 255
+                          ? __builtin_nanf("") : 0.f;
+              else
+                val = (float)reinterpret_cast<const T*>(vr)[col];
               if (!(fabsf(val) < INFINITY)) o[nb][e][i] = fmaf(pk, val, o[nb][e][i]);
             }
         }
@@ -478,7 +575,7 @@ __global__ __launch_bounds__(kThreads) void attend_join(PagedView v, AttendArgs 
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, bool F4 = false>
 int launch(const PagedView& v, const AttendArgs& a, const AttendLists& l, const AttendShape& s,
            hipStream_t st) {
   const unsigned run = (unsigned)std::min(s.seq_tiles, 4);
@@ -488,9 +585,9 @@ int launch(const PagedView& v, const AttendArgs& a, const AttendLists& l, const 
     const int err = launch_attend_many(v, a, l, s, st);
     if (err) return err;
   } else if (s.row_tile == 16) {
-    attend_few<T, D, 1><<<blocks, kThreads, 0, st>>>(v, a, l, run);
+    attend_few<T, D, 1, F4><<<blocks, kThreads, 0, st>>>(v, a, l, run);
   } else if constexpr (sizeof(T) == 2) {
-    attend_few<T, D, 2><<<blocks, kThreads, 0, st>>>(v, a, l, run);
+    attend_few<T, D, 2, F4><<<blocks, kThreads, 0, st>>>(v, a, l, run);
   }
   if (s.n_split > 1) {
     // up to four splits for each thread
@@ -532,6 +629,9 @@ int launch_attend(const PagedView& v, const AttendCall& c, void* stream) {
   AttendLists l;
   l.r = c.r;
   for (int i = 0; i <= c.r.n; ++i) l.tile0[i] = c.tile0[i];
+  if (v.fp4)
+    return v.d == 128 ? launch<__bf16, 128, true>(v, a, l, c.s, st)
+                      : launch<__bf16, 64, true>(v, a, l, c.s, st);
   if (v.esz == 2)
     return v.d == 128 ? launch<__bf16, 128>(v, a, l, c.s, st) : launch<__bf16, 64>(v, a, l, c.s, st);
   return v.d == 128 ? launch<float, 128>(v, a, l, c.s, st) : launch<float, 64>(v, a, l, c.s, st);

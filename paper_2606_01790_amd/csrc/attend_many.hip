@@ -91,7 +91,39 @@ __device__ inline void stage(const char* from, int64_t ts, uint32_t row, uint32_
         (__attribute__((address_space(3))) void*)(to + j * 1024), 16, 0, 0);
 }
 
+// The same of a 4-bit cache, whose elements become bf16 on their way: a lane
+// takes the four bytes of a piece, and the byte of its scale, into registers a
+// step before they go to LDS.
 template <int D>
+struct Fp4Group {
+  static constexpr int kLoads = 16 * D * 2 / 1024, kRows = 16 / kLoads, NP = D / 8;
+  uint32_t w[kLoads];
+  uint8_t s[kLoads];
+  // from: the group's first row, scales: its first scale
+  __device__ __forceinline__ void fetch(const char* from, const char* scales, int lane) {
+    const int at = lane / NP * (D / 32) + lane % NP / 4;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      w[j] = *reinterpret_cast<const uint32_t*>(from + 256 * j + 4 * lane);
+      s[j] = *reinterpret_cast<const uint8_t*>(scales + 16 * j + at);
+    }
+  }
+  // as stage(): `piece` is where the lane's piece lies in instruction 0's row
+  __device__ __forceinline__ void put(uint32_t piece, uint32_t turn, char* to, int lane) const {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const float f = __uint_as_float((uint32_t)s[j] << 23);
+      u32x4 x;
+      x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], f, 0));
+      x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], f, 1));
+      x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], f, 2));
+      x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[j], f, 3));
+      *reinterpret_cast<u32x4*>(to + j * 1024 + lane / NP * (D * 2) + (piece ^ turn * j)) = x;
+    }
+  }
+};
+
+template <int D, bool F4 = false>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_many(PagedView v, AttendArgs a,
                                                               AttendLists s, unsigned run) {
   constexpr int NF = D / 16;               // k-steps of S
@@ -178,6 +210,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_many(PagedView v, Atten
   const auto load_v = [&](uint64_t at, char* to) {
     stage<D>(v.v + at, v.ts, row_off, vpiece, vturn, to + wave * 16 * kRow);
   };
+  // 4 bits: step u + 1's group of V and u + 2's of K, in registers
+  [[maybe_unused]] Fp4Group<D> raw_k, raw_v;
+  [[maybe_unused]] const auto fetch = [&](const char* pool, uint64_t at, int u, Fp4Group<D>& raw) {
+    const int row = (step_token<kStep>(ts, min(u, ts.nt - 1)) + 16 * wave) & (v.P - 1);
+    raw.fetch(pool + at, pool + at + v.P * (D / 2) - row * (D / 2 - D / 32), lane);
+  };
   const auto landed = [&]() {
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     __syncthreads();
@@ -226,14 +264,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_many(PagedView v, Atten
   // 1 fills vn.
   // The addresses of the next rows to stage are worked out beside the products
   // with V, the part of a step that is poorest in other work.
-  uint64_t at1 = 0, at2 = 0;                 // of steps u + 1 and u + 2
+  uint64_t at1 = 0, at2 = 0;                 // of steps u + 1 and u + 2 (4 bits: u + 2 and u + 3)
   unsigned hole0 = 0, hole1 = 0, hole2 = 0;  // groups without a page, of u and the next two
+  [[maybe_unused]] unsigned hole3 = 0;       // (4 bits: three)
   const auto step = [&](int u, const char* kn, char* kf, char* vs, char* vn) {
     // the loads are complete, and every wave is done with what they replace
     landed();
-    if (u + 1 < u1) load_v(at1, vn);
-    if (u + 2 < u1) load_k(at2, kf);
-    const Pages ahead = pages_at(u + 3);
+    if constexpr (F4) {
+      if (u + 1 < u1) raw_v.put(vpiece, vturn, vn + wave * 16 * kRow, lane);
+      if (u + 2 < u1) raw_k.put(kpiece, kturn, kf + wave * 16 * kRow, lane);
+      if (u + 2 < u1) fetch(v.v, at1, u + 2, raw_v);
+      if (u + 3 < u1) fetch(v.k, at2, u + 3, raw_k);
+    } else {
+      if (u + 1 < u1) load_v(at1, vn);
+      if (u + 2 < u1) load_k(at2, kf);
+    }
+    const Pages ahead = pages_at(u + (F4 ? 4 : 3));
 
     const int t0 = step_token<kStep>(ts, u);
     const bool whole = hole0 == 0 && sees_step<kStep>(block, t0);
@@ -373,10 +419,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_many(PagedView v, Atten
     }
     hole0 = hole1;
     hole1 = hole2;
+    if constexpr (F4) hole2 = hole3;
     const auto look_ahead = [&]() {
-      hole2 = holes_of(ahead);
+      (F4 ? hole3 : hole2) = holes_of(ahead);
       at1 = at2;
-      at2 = where(u + 3, ahead);
+      at2 = where(u + (F4 ? 4 : 3), ahead);
     };
     if (idle) {
       look_ahead();
@@ -418,9 +465,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_many(PagedView v, Atten
     const uint64_t at0 = where(u0, p0);
     at1 = where(u0 + 1, p1);
     at2 = where(u0 + 2, p2);
-    load_k(at0, k0);
-    load_v(at0, v0);
-    if (u0 + 1 < u1) load_k(at1, k1);
+    if constexpr (F4) {
+      char* const k_to = k0 + wave * 16 * kRow;
+      fetch(v.k, at0, u0, raw_k);
+      fetch(v.v, at0, u0, raw_v);
+      Fp4Group<D> next;
+      if (u0 + 1 < u1) fetch(v.k, at1, u0 + 1, next);
+      raw_k.put(kpiece, kturn, k_to, lane);
+      raw_v.put(vpiece, vturn, v0 + wave * 16 * kRow, lane);
+      if (u0 + 1 < u1) {
+        next.put(kpiece, kturn, k1 + wave * 16 * kRow, lane);
+        fetch(v.v, at1, u0 + 1, raw_v);
+      }
+      if (u0 + 2 < u1) fetch(v.k, at2, u0 + 2, raw_k);
+      const Pages p3 = pages_at(u0 + 3);
+      hole3 = holes_of(p3);
+      at1 = at2;
+      at2 = where(u0 + 3, p3);
+    } else {
+      load_k(at0, k0);
+      load_v(at0, v0);
+      if (u0 + 1 < u1) load_k(at1, k1);
+    }
     landed();
     if (!idle) {
 #pragma unroll
@@ -469,8 +535,9 @@ int launch_attend_many(const PagedView& v, const AttendArgs& a, const AttendList
   const unsigned run = (unsigned)std::min(s.seq_tiles, 4);
   const unsigned runs = (unsigned)((s.n_tiles + run - 1) / run) * v.n_layers * v.G * s.n_split;
   const unsigned blocks = (runs + 7) / 8 * 8 * run;
-  if (v.d == 128) attend_many<128><<<blocks, 64 * kWaves, 0, st>>>(v, a, l, run);
-  else attend_many<64><<<blocks, 64 * kWaves, 0, st>>>(v, a, l, run);
+  const auto go = [&](auto kernel) { kernel<<<blocks, 64 * kWaves, 0, st>>>(v, a, l, run); };
+  if (v.d == 128) v.fp4 ? go(attend_many<128, true>) : go(attend_many<128>);
+  else v.fp4 ? go(attend_many<64, true>) : go(attend_many<64>);
   return (int)hipGetLastError();
 }
 

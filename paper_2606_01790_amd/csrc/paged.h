@@ -25,6 +25,10 @@ struct PagedView {
   int P, psh;               // page tokens and their logarithm
   int n_pages, n_slots, max_pages;
   int cap;                  // tokens of a table row
+  int row = 0;              // bytes of a K (or V) row in its page
+  // 4 bits: esz is that of q, out and the rows given, bf16.  A block's P rows
+  // are followed, from byte P*row, by their scales, d/32 bytes each
+  bool fp4 = false;
 };
 
 // The sequences of a call, passed to the kernels by value.
@@ -44,6 +48,12 @@ struct RowList {
 };
 
 starkv_status check_paged(const starkv_paged* c, PagedView* v);
+// rows[b] >= 0 query (or written, or read) tokens per sequence, into a list.
+starkv_status take_rows(const PagedView& v, const int32_t* slots, const int32_t* rows, int n,
+                        RowList* r);
+// The strides and addresses of new rows (bytes of an element: v.esz).
+starkv_status check_new_rows(const PagedView& v, const void* k, const void* vv,
+                             const starkv_kv_layout& lay);
 // n slots of the cache, each at most once if `once`.
 starkv_status check_slots(const PagedView& v, const int32_t* slots, int32_t n, bool once);
 
@@ -61,6 +71,8 @@ int launch_pages_grow(const PagedView& v, const SeqList& s, const PagesWs& w, in
                       void* ws, void* stream);
 int launch_pages_write(const PagedView& v, const RowList& r, const void* k, const void* vv,
                        const starkv_kv_layout& lay, void* stream);
+int launch_pages_read(const PagedView& v, const RowList& r, void* k, void* vv,
+                      const starkv_kv_layout& lay, void* stream);
 int launch_pages_fork(const PagedView& v, const SeqList& s, void* stream);
 int launch_pages_free(const PagedView& v, const SeqList& s, int keep_first, int keep_last,
                       void* stream);

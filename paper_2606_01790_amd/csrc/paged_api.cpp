@@ -17,7 +17,8 @@ starkv_status hip_status(int err) { return err ? STARKV_E_HIP : STARKV_OK; }
 
 starkv_status check_paged(const starkv_paged* c, PagedView* v) {
   if (!c) return STARKV_E_NULL;
-  if (c->dtype != STARKV_F32 && c->dtype != STARKV_BF16) return STARKV_E_DTYPE;
+  const bool fp4 = c->dtype == STARKV_FP4;
+  if (c->dtype != STARKV_F32 && c->dtype != STARKV_BF16 && !fp4) return STARKV_E_DTYPE;
   if (c->n_layers < 1 || c->n_layers > 4096) return STARKV_E_SHAPE;
   if (c->G < 1 || c->G > STARKV_MAX_GROUPS || c->H < c->G || c->H % c->G != 0 || c->H > 4096)
     return STARKV_E_SHAPE;
@@ -27,9 +28,9 @@ starkv_status check_paged(const starkv_paged* c, PagedView* v) {
   if (c->n_pages < 1 || c->n_pages > kMaxTokens || c->n_slots < 1 || c->n_slots > (1 << 20) ||
       c->max_pages < 1 || (int64_t)c->max_pages * P > kMaxTokens || c->reserved != 0)
     return STARKV_E_SHAPE;
-  const int64_t esz = c->dtype == STARKV_F32 ? 4 : 2;
+  const int64_t esz = c->dtype == STARKV_F32 ? 4 : fp4 ? 1 : 2;   // of what the strides count
   const int64_t st[4] = {c->layer_stride, c->page_stride, c->group_stride, c->token_stride};
-  if (c->token_stride < c->d) return STARKV_E_SHAPE;
+  if (fp4 ? c->token_stride != c->d / 2 : c->token_stride < c->d) return STARKV_E_SHAPE;
   for (int64_t s : st) {
     if (s < 0 || s > INT64_MAX / 8) return STARKV_E_SHAPE;
     if (s * esz % 16) return STARKV_E_ALIGN;
@@ -52,7 +53,9 @@ starkv_status check_paged(const starkv_paged* c, PagedView* v) {
     v->H = c->H;
     v->G = c->G;
     v->d = c->d;
-    v->esz = (int)esz;
+    v->esz = fp4 ? 2 : (int)esz;
+    v->row = fp4 ? c->d / 2 : c->d * (int)esz;
+    v->fp4 = fp4;
     v->P = P;
     v->psh = 0;
     while ((1 << v->psh) < P) ++v->psh;
@@ -91,9 +94,6 @@ PagesWs pages_ws(const PagedView& v, int n, int64_t most) {
   return w;
 }
 
-namespace {
-
-// rows[b] >= 0 query (or written) tokens per sequence, into a RowList.
 starkv_status take_rows(const PagedView& v, const int32_t* slots, const int32_t* rows, int n,
                         RowList* r) {
   int64_t tot = 0;
@@ -109,7 +109,18 @@ starkv_status take_rows(const PagedView& v, const int32_t* slots, const int32_t*
   return STARKV_OK;
 }
 
-}  // namespace
+starkv_status check_new_rows(const PagedView& v, const void* k, const void* vv,
+                             const starkv_kv_layout& lay) {
+  if (!k || !vv) return STARKV_E_NULL;
+  const int64_t e = v.esz;
+  if (lay.layer_stride > INT64_MAX / 8 || lay.group_stride > INT64_MAX / 8 ||
+      lay.token_stride > INT64_MAX / 8)
+    return STARKV_E_SHAPE;
+  if (lay.layer_stride * e % 16 || lay.group_stride * e % 16 || lay.token_stride * e % 16 ||
+      !at(k, 16) || !at(vv, 16))
+    return STARKV_E_ALIGN;
+  return STARKV_OK;
+}
 
 namespace {
 
@@ -261,14 +272,8 @@ starkv_status write(const starkv_paged* cache, const int32_t* slots, int32_t n,
   if (lay->layer_stride < 0 || lay->group_stride < 0 || lay->token_stride < 0)
     return STARKV_E_SHAPE;
   if (r.row0[n] == 0) return STARKV_OK;
-  if (!k || !vv) return STARKV_E_NULL;
-  const int64_t e = v.esz;
-  if (lay->layer_stride > INT64_MAX / 8 || lay->group_stride > INT64_MAX / 8 ||
-      lay->token_stride > INT64_MAX / 8)
-    return STARKV_E_SHAPE;
-  if (lay->layer_stride * e % 16 || lay->group_stride * e % 16 || lay->token_stride * e % 16 ||
-      !at(k, 16) || !at(vv, 16) || !at(grown, 4))
-    return STARKV_E_ALIGN;
+  if ((st = check_new_rows(v, k, vv, *lay)) != STARKV_OK) return st;
+  if (!at(grown, 4)) return STARKV_E_ALIGN;
   return hip_status(launch_pages_write(v, r, k, vv, *lay, stream));
 }
 

@@ -202,6 +202,19 @@ __global__ __launch_bounds__(kPlanThreads) void grow_plan(PagedView v, Seqs<N> s
   }
 }
 
+// 4-bit caches are those whose rows are two or four vectors: their scales, as
+// many bytes, lie behind the block's rows and move along.
+template <int VPR>
+struct ScaleRow {
+  using type = uint32_t;
+};
+template <>
+struct ScaleRow<2> {
+  using type = uint16_t;
+};
+template <int VPR>
+constexpr bool kScaled = VPR <= 4;
+
 // Rows [0, part) of a replaced page, one (sequence, group, layer) per block (16
 // forks with 28 or 35 rows in 28 layers: 10.4 us, 5.6 TB/s read and written;
 // with nothing to copy 2).
@@ -217,6 +230,16 @@ __global__ __launch_bounds__(256) void grow_copy(PagedView v, const i32x4* info)
     const i32x4 vv = *reinterpret_cast<const i32x4*>(v.v + from + off);
     *reinterpret_cast<i32x4*>(v.k + to + off) = kk;
     *reinterpret_cast<i32x4*>(v.v + to + off) = vv;
+  }
+  if constexpr (kScaled<VPR>) {
+    using S = typename ScaleRow<VPR>::type;
+    for (int i = threadIdx.x; i < c[2]; i += 256) {
+      const int64_t off = (int64_t)v.P * v.row + (int64_t)i * sizeof(S);
+      const S ks = *reinterpret_cast<const S*>(v.k + from + off);
+      const S vs = *reinterpret_cast<const S*>(v.v + from + off);
+      *reinterpret_cast<S*>(v.k + to + off) = ks;
+      *reinterpret_cast<S*>(v.v + to + off) = vs;
+    }
   }
 }
 
@@ -252,6 +275,116 @@ __global__ __launch_bounds__(256) void write_kernel(PagedView v, Rows<N> r, Writ
                        (int64_t)(t & (v.P - 1)) * v.ts + part * 16;
     *reinterpret_cast<i32x4*>(v.k + to) = *reinterpret_cast<const i32x4*>(a.k + from);
     *reinterpret_cast<i32x4*>(v.v + to) = *reinterpret_cast<const i32x4*>(a.v + from);
+  }
+}
+
+// The same into a 4-bit cache: a thread takes 16 bytes, eight elements, of K and
+// of V, and four neighbours the 32 elements that share a scale.  Their largest
+// magnitude, as an integer (which orders infinities and NaN above all numbers),
+// gives the scale by its exponent, one more where the mantissa is over 1.75; the
+// hardware's conversion divides by it, exactly, and rounds to the nearest, ties to
+// the even code.
+__device__ inline uint32_t quad_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true));   // lanes 1 0 3 2
+  return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));  // lanes 2 3 0 1
+}
+__device__ inline uint32_t quantise(const i32x4& x, uint32_t* scale) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  uint32_t top = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+    top = max(top, max((uint32_t)x[w] << 16 & 0x7FFF0000u, (uint32_t)x[w] & 0x7FFF0000u));
+  top = quad_max(top);
+  const uint32_t byte = min(max((int)((top + 0x1FFFFFu) >> 23) - 2, 2), 252);
+  *scale = top >= 0x7F800000u ? 255u : byte;
+  const float s = __uint_as_float(byte << 23);
+  uint32_t code = 0;
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2, (uint32_t)x[0]), s, 0);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2, (uint32_t)x[1]), s, 1);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2, (uint32_t)x[2]), s, 2);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2, (uint32_t)x[3]), s, 3);
+  return code;
+}
+
+template <int D, int N>
+__global__ __launch_bounds__(256) void write_fp4(PagedView v, Rows<N> r, WriteArgs a) {
+  constexpr int VPR = D / 8;
+  const int64_t n = (int64_t)r.row0[r.n] * v.G * VPR;
+  const int layer = blockIdx.y;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int part = (int)(i % VPR);
+    const int64_t rg = i / VPR;
+    const int g = (int)(rg % v.G), row = (int)(rg / v.G);
+    const int b = owner_of(r.row0, r.n, row);
+    if (a.grown && a.grown[b] != STARKV_SEQ_OK) continue;
+    const int t = seq_len(v, r.slot[b]) - r.row0[b + 1] + row;
+    if (t < 0) continue;
+    const int page = table_row(v, r.slot[b])[t >> v.psh];
+    if (!is_page(v, page) || v.refs[page] > 1) continue;
+    const int64_t from = (int64_t)layer * a.ls + (int64_t)g * a.gs + (int64_t)row * a.ts + part * 16;
+    const int64_t block = (int64_t)layer * v.ls + (int64_t)page * v.ps + (int64_t)g * v.gs;
+    const int in_page = t & (v.P - 1);
+    const int64_t to = block + (int64_t)in_page * (D / 2) + part * 4;
+    const int64_t sto = block + (int64_t)v.P * (D / 2) + in_page * (D / 32) + part / 4;
+    uint32_t ks, vs;
+    const uint32_t kc = quantise(*reinterpret_cast<const i32x4*>(a.k + from), &ks);
+    const uint32_t vc = quantise(*reinterpret_cast<const i32x4*>(a.v + from), &vs);
+    *reinterpret_cast<uint32_t*>(v.k + to) = kc;
+    *reinterpret_cast<uint32_t*>(v.v + to) = vc;
+    if (part % 4 == 0) {
+      v.k[sto] = (char)ks;
+      v.v[sto] = (char)vs;
+    }
+  }
+}
+
+// The rows of tokens out of their pages, 16 bytes of K and of V per thread; of a
+// 4-bit cache the bf16 numbers that four bytes stand for.  What has no page gives
+// zeros.
+struct ReadArgs {
+  char* k;
+  char* v;
+  int64_t ls, gs, ts;   // byte strides
+};
+__device__ inline i32x4 dequantise(uint32_t w, uint32_t byte) {
+  const float s = __uint_as_float(byte << 23);
+  return i32x4{__builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0)),
+               __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1)),
+               __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2)),
+               __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3))};
+}
+// VPR: 16-byte vectors of a row in the pool
+template <int VPR, int N>
+__global__ __launch_bounds__(256) void read_kernel(PagedView v, Rows<N> r, ReadArgs a) {
+  constexpr bool F4 = kScaled<VPR>;
+  constexpr int kOut = F4 ? 4 * VPR : VPR;     // vectors of a row given back
+  const int64_t n = (int64_t)r.row0[r.n] * v.G * kOut;
+  const int layer = blockIdx.y;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int part = (int)(i % kOut);
+    const int64_t rg = i / kOut;
+    const int g = (int)(rg % v.G), row = (int)(rg / v.G);
+    const int b = owner_of(r.row0, r.n, row);
+    const int t = seq_len(v, r.slot[b]) - r.row0[b + 1] + row;
+    const int page = t < 0 ? -1 : table_row(v, r.slot[b])[t >> v.psh];
+    i32x4 kk{0, 0, 0, 0}, vv{0, 0, 0, 0};
+    if (is_page(v, page)) {
+      const int64_t block = (int64_t)layer * v.ls + (int64_t)page * v.ps + (int64_t)g * v.gs;
+      const int in_page = t & (v.P - 1);
+      if constexpr (F4) {
+        const int64_t from = block + (int64_t)in_page * (16 * VPR) + part * 4;
+        const int64_t at = block + (int64_t)v.P * (16 * VPR) + in_page * VPR + part / 4;
+        kk = dequantise(*reinterpret_cast<const uint32_t*>(v.k + from), (uint8_t)v.k[at]);
+        vv = dequantise(*reinterpret_cast<const uint32_t*>(v.v + from), (uint8_t)v.v[at]);
+      } else {
+        const int64_t from = block + (int64_t)in_page * v.ts + part * 16;
+        kk = *reinterpret_cast<const i32x4*>(v.k + from);
+        vv = *reinterpret_cast<const i32x4*>(v.v + from);
+      }
+    }
+    const int64_t to = (int64_t)layer * a.ls + (int64_t)g * a.gs + (int64_t)row * a.ts + part * 16;
+    *reinterpret_cast<i32x4*>(a.k + to) = kk;
+    *reinterpret_cast<i32x4*>(a.v + to) = vv;
   }
 }
 
@@ -436,6 +569,22 @@ __global__ __launch_bounds__(256) void compact_move(PagedView v, Seqs<N> s, Move
     const int64_t to = base + (int64_t)row[r >> v.psh] * v.ps + (int64_t)(r & (v.P - 1)) * v.ts + part * 16;
     __builtin_nontemporal_store(kk, reinterpret_cast<i32x4*>(v.k + to));
     __builtin_nontemporal_store(vv, reinterpret_cast<i32x4*>(v.v + to));
+    if constexpr (kScaled<VPR>) {
+      if (part == 0) {
+        using S = typename ScaleRow<VPR>::type;
+        S ks = 0, vs = 0;
+        if (is_page(v, page)) {
+          const int64_t from = base + (int64_t)page * v.ps + (int64_t)v.P * v.row +
+                               (int64_t)(t & (v.P - 1)) * sizeof(S);
+          ks = *reinterpret_cast<const S*>(v.k + from);
+          vs = *reinterpret_cast<const S*>(v.v + from);
+        }
+        const int64_t sto = base + (int64_t)row[r >> v.psh] * v.ps + (int64_t)v.P * v.row +
+                            (int64_t)(r & (v.P - 1)) * sizeof(S);
+        *reinterpret_cast<S*>(v.k + sto) = ks;
+        *reinterpret_cast<S*>(v.v + sto) = vs;
+      }
+    }
   }
 }
 
@@ -444,7 +593,9 @@ using Int = std::integral_constant<int, I>;
 // f(16-byte vectors of a row), f(the call's list)
 template <typename F>
 void by_row_vectors(const PagedView& v, F f) {
-  switch (v.d * v.esz / 16) {
+  switch (v.row / 16) {
+    case 2: f(Int<2>{}); break;
+    case 4: f(Int<4>{}); break;
     case 8: f(Int<8>{}); break;
     case 16: f(Int<16>{}); break;
     default: f(Int<32>{}); break;
@@ -489,11 +640,34 @@ int launch_pages_write(const PagedView& v, const RowList& r, const void* k, cons
   WriteArgs a{static_cast<const char*>(k), static_cast<const char*>(vv), lay.layer_stride * v.esz,
               lay.group_stride * v.esz, lay.token_stride * v.esz, r.grown};
   const int64_t nvec = (int64_t)r.row0[r.n] * v.G * (v.d * v.esz / 16);
-  const unsigned blocks = (unsigned)std::min((nvec + 255) / 256, kMaxBlocks);
+  const dim3 grid((unsigned)std::min((nvec + 255) / 256, kMaxBlocks), v.n_layers);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (v.fp4) {
+    with_list(r, [&](const auto& l) {
+      if (v.d == 128) write_fp4<128><<<grid, 256, 0, st>>>(v, l, a);
+      else write_fp4<64><<<grid, 256, 0, st>>>(v, l, a);
+    });
+    return (int)hipGetLastError();
+  }
+  by_row_vectors(v, [&](auto vpr) {
+    if constexpr (!kScaled<decltype(vpr)::value>)
+      with_list(r, [&](const auto& l) {
+        write_kernel<decltype(vpr)::value><<<grid, 256, 0, st>>>(v, l, a);
+      });
+  });
+  return (int)hipGetLastError();
+}
+
+int launch_pages_read(const PagedView& v, const RowList& r, void* k, void* vv,
+                      const starkv_kv_layout& lay, void* stream) {
+  ReadArgs a{static_cast<char*>(k), static_cast<char*>(vv), lay.layer_stride * v.esz,
+             lay.group_stride * v.esz, lay.token_stride * v.esz};
+  const int64_t nvec = (int64_t)r.row0[r.n] * v.G * (v.d * v.esz / 16);
+  const dim3 grid((unsigned)std::min((nvec + 255) / 256, kMaxBlocks), v.n_layers);
   by_row_vectors(v, [&](auto vpr) {
     with_list(r, [&](const auto& l) {
-      write_kernel<decltype(vpr)::value>
-          <<<dim3(blocks, v.n_layers), 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(v, l, a);
+      read_kernel<decltype(vpr)::value>
+          <<<grid, 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(v, l, a);
     });
   });
   return (int)hipGetLastError();
@@ -534,7 +708,7 @@ int launch_pages_compact(const PagedView& v, const SeqList& s, bool whole, const
   });
   if (B + tail > 0) {
     // the most rows of a sequence: the kept ones and the first page's before them
-    const int vpr_n = v.d * v.esz / 16;
+    const int vpr_n = v.row / 16;
     const int64_t nvec = ((int64_t)B + tail + v.P - 1) * vpr_n;
     const int64_t per = (int64_t)s.n * v.G;      // at most 2^14
     m.chunks = (int)std::min<int64_t>({(nvec + 255) / 256, kMaxBlocks / per, 65535});

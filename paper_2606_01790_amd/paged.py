@@ -22,7 +22,8 @@ from .starkv import KVLayout, StarKVError
 MAX_SEQS = 256
 MAX_DRAFT_WORDS = 4
 MAX_TOKENS = 1 << 26
-SEQ_OK, SEQ_NO_PAGES, SEQ_RANGE = 0, 1, 2
+SEQ_OK, SEQ_NO_PAGES, SEQ_RANGE, SEQ_SHORT = 0, 1, 2, 3
+FP4 = 4                  # the dtype of a cache held in 4 bits
 
 
 class Paged(ctypes.Structure):
@@ -46,6 +47,8 @@ SIGNATURES = {
                                      c_void_p]),
     "starkv_pages_write_grown": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, _L,
                                            c_void_p, c_void_p]),
+    "starkv_pages_read": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, _L,
+                                    c_void_p]),
     "starkv_pages_fork": (c_int32, [_P, c_void_p, c_void_p, c_int32, c_void_p]),
     "starkv_pages_free": (c_int32, [_P, c_void_p, c_int32, c_int32, c_int32, c_void_p]),
     "starkv_pages_compact": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_void_p, c_int64, c_int32,
@@ -60,6 +63,13 @@ SIGNATURES = {
     "starkv_attend_window": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_int32,
                                        c_int32, c_void_p, c_void_p, c_void_p, c_size_t,
                                        c_void_p]),
+    "starkv_mass_add": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_int32,
+                                  c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "starkv_mass_workspace_bytes": (c_size_t, [_P, c_void_p, c_int32, c_int32]),
+    "starkv_mass_fork": (c_int32, [_P, c_void_p, c_void_p, c_int32, c_void_p, c_void_p]),
+    "starkv_pages_evict": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_int32, c_int32, c_int32,
+                                     c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "starkv_evict_workspace_bytes": (c_size_t, [_P, c_int32, c_int32, c_int32, c_int32]),
 }
 
 _lib = None
@@ -91,18 +101,31 @@ class Cache:
     """A pool's tensors and the struct that every call takes.
 
     k, v:   [n_layers, n_pages, G, page_tokens, d], bfloat16 or float32, any
-            strides (the same for both) with a unit last one
+            strides (the same for both) with a unit last one; or, held in 4 bits,
+            [n_layers, n_pages, G, fp4_block_bytes(page_tokens, d)] uint8, and then d
     table:  [n_slots, max_pages] int32;  length: [n_slots] int32;
     refs:   [n_pages] int32; all three contiguous
     H:      query heads
     """
 
-    def __init__(self, k, v, table, length, refs, H: int):
-        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.stride(4) != 1:
+    def __init__(self, k, v, table, length, refs, H: int, d: int | None = None):
+        fp4 = k.dtype == torch.uint8
+        if fp4:
+            if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1:
+                raise ValueError("k and v: [n_layers, n_pages, G, bytes] of the same strides, the last "
+                                 "one 1")
+            if d not in (64, 128):
+                raise ValueError(f"d: {d}, 64 or 128 required with a cache of 4 bits")
+            P = k.shape[3] // fp4_block_bytes(1, d)
+            if k.shape[3] != fp4_block_bytes(P, d):
+                raise ValueError(f"k: blocks of {k.shape[3]} bytes, no rows of {fp4_block_bytes(1, d)}")
+        elif k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.stride(4) != 1:
             raise ValueError("k and v: [n_layers, n_pages, G, page_tokens, d] of the same strides, "
                              "the last one 1")
-        if k.dtype not in (torch.bfloat16, torch.float32):
-            raise ValueError(f"k: {k.dtype}, bfloat16 or float32 required")
+        elif d is not None and d != k.shape[4]:
+            raise ValueError(f"d: {d}, rows of {k.shape[4]}")
+        if k.dtype not in (torch.bfloat16, torch.float32, torch.uint8):
+            raise ValueError(f"k: {k.dtype}, bfloat16 or float32 required (uint8: 4 bits)")
         _tensor(k, k.dtype, "k")
         _tensor(v, k.dtype, "v", k.device)
         for t, n, what in ((table, 2, "table"), (length, 1, "length"), (refs, 1, "refs")):
@@ -112,14 +135,19 @@ class Cache:
         if length.shape[0] != table.shape[0] or refs.shape[0] != k.shape[1]:
             raise ValueError("length: one per row of table; refs: one per page")
         self.k, self.v, self.table, self.length, self.refs = k, v, table, length, refs
-        self.device, self.dtype = k.device, k.dtype
-        nl, n_pages, G, P, d = k.shape
-        sl, sp, sg, st, _ = k.stride()
+        # dtype: of q, out, and the rows written and read
+        self.device, self.dtype, self.fp4 = k.device, torch.bfloat16 if fp4 else k.dtype, fp4
+        if fp4:
+            nl, n_pages, G, _ = k.shape
+            (sl, sp, sg, _), st = k.stride(), d // 2
+        else:
+            nl, n_pages, G, P, d = k.shape
+            sl, sp, sg, st, _ = k.stride()
         self.n_layers, self.H, self.G, self.d, self.page_tokens = nl, H, G, d, P
         self.cap = table.shape[1] * P
-        self.c = Paged(nl, H, G, d, sk.F32 if k.dtype == torch.float32 else sk.BF16, P, n_pages,
-                       table.shape[0], table.shape[1], 0, sl, sp, sg, st, k.data_ptr(),
-                       v.data_ptr(), table.data_ptr(), length.data_ptr(), refs.data_ptr())
+        dtype = FP4 if fp4 else sk.F32 if k.dtype == torch.float32 else sk.BF16
+        self.c = Paged(nl, H, G, d, dtype, P, n_pages, table.shape[0], table.shape[1], 0, sl, sp,
+                       sg, st, k.data_ptr(), v.data_ptr(), table.data_ptr(), length.data_ptr(), refs.data_ptr())
         self.ref = ctypes.byref(self.c)
 
     def layers(self, first: int, count: int = 1) -> "Cache":
@@ -129,16 +157,26 @@ class Cache:
         k = self.k[first:first + count]
         if count < 1 or k.shape[0] != count:     # a slice of fewer would pass for the whole
             raise ValueError(f"layers [{first}, {first + count}) of {self.n_layers}")
-        return Cache(k, self.v[first:first + count], self.table, self.length, self.refs, self.H)
+        return Cache(k, self.v[first:first + count], self.table, self.length, self.refs, self.H, self.d)
+
+
+def fp4_block_bytes(page_tokens: int, d: int) -> int:
+    """Of a page's K (or V) of one layer and group in 4 bits: rows and scales."""
+    return page_tokens * (d // 2 + d // 32)
 
 
 def new_cache(n_layers: int, n_pages: int, page_tokens: int, G: int, d: int, n_slots: int,
               max_pages: int, H: int, dtype=torch.bfloat16, device="cuda") -> Cache:
-    """A pool of its own tensors, made empty."""
-    k = torch.empty(n_layers, n_pages, G, page_tokens, d, dtype=dtype, device=device)
+    """A pool of its own tensors, made empty.  dtype: torch.bfloat16, torch.float32,
+    or FP4 for a cache held in 4 bits."""
+    if dtype == FP4:
+        k = torch.empty(n_layers, n_pages, G, fp4_block_bytes(page_tokens, d), dtype=torch.uint8,
+                        device=device)
+    else:
+        k = torch.empty(n_layers, n_pages, G, page_tokens, d, dtype=dtype, device=device)
     i32 = dict(dtype=torch.int32, device=device)
     c = Cache(k, torch.empty_like(k), torch.empty(n_slots, max_pages, **i32),
-              torch.empty(n_slots, **i32), torch.empty(n_pages, **i32), H)
+              torch.empty(n_slots, **i32), torch.empty(n_pages, **i32), H, d)
     pages_init(c)
     return c
 
@@ -222,12 +260,7 @@ def pages_grow(cache: Cache, slots, add, status, ws, stream=None):
          _bytes(ws))
 
 
-def pages_write(cache: Cache, slots, rows, k, v, layout: KVLayout, stream=None, grown=None):
-    """k, v: K and V of the sequences' new tokens, `layout` over (layer, group,
-    row): rows_layout of a [n_layers, rows, G, d] tensor, or contiguous_layout
-    of a compacted cache's [n_layers, G, rows, d].  grown: the status of the
-    pages_grow of the same slots that made the tokens (starkv_pages_write_grown):
-    a sequence that it left unchanged stays so."""
+def _check_rows(cache, slots, rows, k, v, layout):
     n, tot = len(slots), sum(rows)
     if len(rows) != n:
         raise ValueError("rows: one number per slot")
@@ -238,12 +271,27 @@ def pages_write(cache: Cache, slots, rows, k, v, layout: KVLayout, stream=None, 
         have = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
         if tot and have < last:
             raise ValueError(f"{what}: {have} elements < {last} required")
-    args = (_ints(slots), n, _ints(rows), _ptr(k), _ptr(v), ctypes.byref(layout))
+    return _ints(slots), n, _ints(rows), _ptr(k), _ptr(v), ctypes.byref(layout)
+
+
+def pages_write(cache: Cache, slots, rows, k, v, layout: KVLayout, stream=None, grown=None):
+    """k, v: K and V of the sequences' new tokens, `layout` over (layer, group,
+    row): rows_layout of a [n_layers, rows, G, d] tensor, or contiguous_layout
+    of a compacted cache's [n_layers, G, rows, d].  grown: the status of the
+    pages_grow of the same slots that made the tokens (starkv_pages_write_grown):
+    a sequence that it left unchanged stays so."""
+    args = _check_rows(cache, slots, rows, k, v, layout)
     if grown is None:
         _run("starkv_pages_write", cache, stream, *args)
     else:
-        _int32(grown, n, "grown", cache.device)
+        _int32(grown, len(slots), "grown", cache.device)
         _run("starkv_pages_write_grown", cache, stream, *args, _ptr(grown))
+
+
+def pages_read(cache: Cache, slots, rows, k, v, layout: KVLayout, stream=None):
+    """K and V of the sequences' last tokens into k and v, laid out as for
+    pages_write."""
+    _run("starkv_pages_read", cache, stream, *_check_rows(cache, slots, rows, k, v, layout))
 
 
 def pages_fork(cache: Cache, src, dst, stream=None):
@@ -327,3 +375,68 @@ def attend_window(cache: Cache, slots, rows, q, window: int, sinks: int, out, ws
     n, _ = _attend_args(cache, slots, rows, q, out, lse, ws)
     _run("starkv_attend_window", cache, stream, _ints(slots), n, _ints(rows), _ptr(q), window, sinks,
          cache.cap if max_len is None else max_len, _ptr(out), _ptr(lse), _ptr(ws), _bytes(ws))
+
+
+# ------------------------------------------------------------------ accumulated weights
+
+def new_mass(cache: Cache):
+    """Masses of the cache's tokens, all zero: [n_layers, n_slots, tokens of a table
+    row]."""
+    return torch.zeros(cache.n_layers, cache.table.shape[0], cache.cap, device=cache.device)
+
+
+def _mass(t, cache, what):
+    _tensor(t, torch.float32, what, cache.device)
+    shape = (cache.n_layers, cache.table.shape[0], cache.cap)
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous {shape} required, got {tuple(t.shape)}")
+
+
+def mass_workspace_bytes(cache: Cache, rows, max_len: int) -> int:
+    rows = _ints(rows)
+    return int(lib().starkv_mass_workspace_bytes(cache.ref, rows.buffer_info()[0], len(rows), max_len))
+
+
+def mass_add(cache: Cache, slots, rows, q, lse, window: int, sinks: int, mass, out, ws,
+             max_len: int | None = None, stream=None):
+    """q, window, sinks: of an attend_window call, lse: what it gave.  mass, out:
+    [n_layers, n_slots, tokens of a table row], of new_mass; a view of layers takes
+    the same layers of both.  out may be mass."""
+    n, tot = len(slots), sum(rows)
+    if len(rows) != n:
+        raise ValueError("rows: one number per slot")
+    need = cache.n_layers * tot * cache.H
+    for t, count, dtype, what in ((q, need * cache.d, cache.dtype, "q"),
+                                  (lse, need, torch.float32, "lse")):
+        _tensor(t, dtype, what, cache.device)
+        if not t.is_contiguous() or t.numel() < count:
+            raise ValueError(f"{what}: {count} contiguous elements required")
+    _mass(mass, cache, "mass")
+    _mass(out, cache, "out")
+    _buffer(ws, 0, "ws", cache.device)
+    _run("starkv_mass_add", cache, stream, _ints(slots), n, _ints(rows), _ptr(q), _ptr(lse), window,
+         sinks, cache.cap if max_len is None else max_len, _ptr(mass), _ptr(out), _ptr(ws), _bytes(ws))
+
+
+def mass_fork(cache: Cache, src, dst, mass, stream=None):
+    if len(src) != len(dst):
+        raise ValueError("src and dst: one slot each per fork")
+    _mass(mass, cache, "mass")
+    _run("starkv_mass_fork", cache, stream, _ints(src), _ints(dst), len(src), _ptr(mass))
+
+
+def evict_workspace_bytes(cache: Cache, n: int, keep: int, sinks: int, recent: int) -> int:
+    return int(lib().starkv_evict_workspace_bytes(cache.ref, n, keep, sinks, recent))
+
+
+def pages_evict(cache: Cache, slots, mass, keep: int, sinks: int, recent: int, idx, status, ws,
+                stream=None):
+    """idx: [n_layers, n, sinks + keep] int32, out: the tokens kept of each sequence
+    but for the recent ones."""
+    n = len(slots)
+    _mass(mass, cache, "mass")
+    _int32(idx, cache.n_layers * n * (max(sinks, 0) + max(keep, 0)), "idx", cache.device)
+    _int32(status, n, "status", cache.device)
+    _buffer(ws, 0, "ws", cache.device)
+    _run("starkv_pages_evict", cache, stream, _ints(slots), n, _ptr(mass), keep, sinks, recent,
+         _ptr(idx), _ptr(status), _ptr(ws), _bytes(ws))
