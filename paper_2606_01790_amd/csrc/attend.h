@@ -22,13 +22,6 @@ struct AttendArgs {
   float scale;            // log2(e) / sqrt(d)
 };
 
-// Tables and lengths do not change while a kernel reads them: uniform reads go
-// through the scalar cache.
-typedef __attribute__((address_space(4))) int32_t const_i32;
-__device__ inline const const_i32* const_ints(const int32_t* p) {
-  return (const const_i32*)(uintptr_t)p;
-}
-
 struct AttendLists {      // with PagedView and AttendArgs below 4 KB of kernel arguments
   RowList r;
   int32_t tile0[kMaxSeqs + 1];

@@ -14,6 +14,13 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWave = 64;
 
+// Tables and lengths do not change while a kernel reads them: uniform reads go
+// through the scalar cache.
+typedef __attribute__((address_space(4))) int32_t const_i32;
+__device__ inline const const_i32* const_ints(const int32_t* p) {
+  return (const const_i32*)(uintptr_t)p;
+}
+
 // 32x32 MFMA tiles.  For v_mfma_f32_32x32x16_bf16 / _32x32x2f32, lane l
 // supplies row (l % 32) of A and column (l % 32) of B with the k-slice of
 // half h = l / 32, and receives the 16 accumulators

@@ -6,15 +6,17 @@
 
 namespace starkv {
 
-// How a call that adds weights is divided: `blocks` blocks of each (layer,
-// sequence) take its token tiles in turn; in the kernel for many rows n_split of
-// them share a tile's products, and their sums are joined afterwards.
+// How a call that adds weights is divided.  Few rows: `blocks` blocks take the tiles
+// of all sequences and layers in turn.  Many rows: `blocks` of each (layer,
+// sequence) take its tiles in turn, n_split of them share a tile's products, and
+// their sums are joined afterwards.
 struct MassShape {
   bool many;       // the kernel for many rows
   int n_rows;      // query tokens of the call
   int tile;        // tokens of a tile
   int tiles;       // tiles of a sequence, by the bound on the lengths
-  int blocks;      // of a (layer, sequence), for each split
+  int row_blocks;  // few rows: 16-row blocks of a group, at most
+  int blocks;
   int n_split;
   size_t ws_bytes; // the splits' sums, float [n_layers][n][n_split][tiles*tile]
 };

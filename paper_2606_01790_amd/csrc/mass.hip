@@ -10,8 +10,8 @@
 // the last) spoils no other token.
 //
 // Few rows (a decoded token, a few drafted ones; float32 of any number) are bound
-// by HBM: mass_few takes 64 tokens a block, K straight to registers, four items of
-// 16 tokens of a group to a wave and a group; the groups are added up through LDS.
+// by HBM: mass_few takes tiles of 64 tokens, K straight to registers, and adds up the
+// groups through LDS.
 // Many rows are bound by the matrix units and the exponentials: mass_many keeps 64
 // tokens' K in a wave's registers and walks the rows, which all waves read from
 // LDS, groups one after the other into the same sums.
@@ -44,32 +44,29 @@ struct Seq {
   int n, T, first;          // length, query tokens, position of the first (may be negative)
   int row0, hpg, R;         // its first row of the call; heads, and rows, of a group
   const int32_t* table;
-  const float* mass;
-  float* out;
+  size_t at;                // its first mass
 };
-__device__ inline Seq seq_of(const PagedView& v, const MassArgs& a, const RowList& r, int layer,
-                             int b) {
+__device__ inline Seq seq_of(const PagedView& v, const RowList& r, int layer, int b) {
   Seq s;
   const int slot = r.slot[b];
-  s.n = min(max(v.len[slot], 0), v.cap);
+  s.n = min(max(const_ints(v.len)[slot], 0), v.cap);
   s.row0 = r.row0[b];
   s.T = r.row0[b + 1] - s.row0;
   s.first = s.n - s.T;
   s.hpg = v.H / v.G;
   s.R = s.T * s.hpg;
   s.table = v.table + (size_t)slot * v.max_pages;
-  const size_t at = ((size_t)layer * v.n_slots + slot) * v.cap;
-  s.mass = a.mass + at;
-  s.out = a.out + at;
+  s.at = ((size_t)layer * v.n_slots + slot) * v.cap;
   return s;
 }
 __device__ inline bool is_page(const PagedView& v, int p) { return p >= 0 && p < v.n_pages; }
 
 // Token t's mass with what the rows add to it (nothing to a dropped token,
 // whatever was computed in its place).
-__device__ inline void store_mass(const PagedView& v, const Seq& s, int t, float add) {
-  const float old = t < s.first ? s.mass[t] : 0.f;
-  s.out[t] = is_page(v, s.table[t >> v.psh]) ? old + add : old;
+__device__ inline void store_mass(const PagedView& v, const MassArgs& a, const Seq& s, int t,
+                                  float add) {
+  const float old = t < s.first ? a.mass[s.at + t] : 0.f;
+  a.out[s.at + t] = is_page(v, s.table[t >> v.psh]) ? old + add : old;
 }
 // Whether any row sees any of the tokens [t0, t1).
 __device__ inline bool any_sees(const MassArgs& a, const Seq& s, int t0, int t1) {
@@ -145,78 +142,187 @@ struct KRow<__bf16, D, true> {
   __device__ static inline int q_byte(int i, int quad) { return quad * (D / 2) + 16 * i; }
 };
 
-// 16-token parts of a group: a wave takes G of the tile's 4*G, whole groups where
-// there are four or more.
+// What 16 rows of a group are to a lane: its part of row l16 of Q, and of rows 4*quad
+// + e the log-sum and the position (-1: sees nothing).
 template <typename T, int D, bool F4>
-__global__ __launch_bounds__(kThreads) void mass_few(PagedView v, MassArgs a, RowList r) {
-  using F = Frag<T>;
-  using frag = typename F::type;
+struct Rows16 {
   using K = KRow<T, D, F4>;
-  extern __shared__ float sums[];       // [G][64]
+  typename Frag<T>::type q[K::NF];
+  float l[4];
+  int p[4];
+  __device__ inline void load(const PagedView& v, const MassArgs& a, const Seq& s, int layer, int g,
+                              int r0) {
+    const int l16 = threadIdx.x & 15, quad = threadIdx.x >> 4 & 3;
+    const size_t at = ((size_t)layer * a.n_rows + s.row0) * v.H + g * s.hpg;
+    const int mine = min(r0 + l16, s.R - 1), i = mine / s.hpg;
+    const char* qr = a.q + (at + (size_t)i * v.H + (mine - i * s.hpg)) * D * sizeof(T);
+#pragma unroll
+    for (int f = 0; f < K::NF; ++f)
+      q[f] = *reinterpret_cast<const typename Frag<T>::type*>(qr + K::q_byte(f, quad));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int row = r0 + 4 * quad + e, r = min(row, s.R - 1), qi = r / s.hpg;
+      const float lse = a.lse[at + (size_t)qi * v.H + (r - qi * s.hpg)];
+      l[e] = lse * kLog2e;
+      p[e] = row < s.R && lse != -INFINITY ? s.first + qi : -1;
+    }
+  }
+  // The lane's rows' weights of token t, whose part of K the lane holds.
+  __device__ inline float weigh(const MassArgs& a, const K& k, int t) const {
+    f32x4 x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int f = 0; f < K::NF; ++f) x = Frag<T>::mma(q[f], k.get(f), x);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float w = __builtin_amdgcn_exp2f(fmaf(x[e], a.scale, -l[e]));
+      sum += sees(a, p[e], t) ? w : 0.f;
+    }
+    return sum;
+  }
+};
+
+// The token tiles of a call, of kTokens each: those of its sequences in order, layer
+// by layer; a block takes every gridDim.x-th, so that all have as many whatever the
+// lengths are.  The lanes of a wave know how many tiles come before each sequence.
+template <int kTokens>
+struct Tiles {
+  static constexpr int kPer = kMaxSeqs / 64;
+  int before[kPer], count[kPer];
+  int all;                   // tiles of a layer
+  int next = blockIdx.x;     // the block's next one, in layer `layer`
+  int layer = 0;
+
+  __device__ inline Tiles(const PagedView& v, const RowList& r) {
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int i = kPer * (threadIdx.x & 63) + j;
+      count[j] = 0;
+      if (i < r.n && r.row0[i + 1] > r.row0[i])
+        count[j] = (min(max(v.len[r.slot[i]], 0), v.cap) + kTokens - 1) / kTokens;
+      mine += count[j];
+    }
+    const int inc = wave_incl_scan(mine);
+    all = __builtin_amdgcn_readlane(inc, 63);
+    before[0] = inc - mine;
+#pragma unroll
+    for (int j = 1; j < kPer; ++j) before[j] = before[j - 1] + count[j - 1];
+  }
+  // The block's next tile that rows see, into b and t0; the others keep their
+  // masses.  False when there is none.
+  __device__ inline bool take(const PagedView& v, const MassArgs& a, const RowList& r, int* at_layer,
+                              Seq* s, int* b, int* t0) {
+    if (all == 0) return false;
+    for (;; next += gridDim.x) {
+      while (next >= all) {
+        next -= all;
+        if (++layer >= v.n_layers) return false;
+      }
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        const uint64_t hit = __ballot(before[j] <= next && next < before[j] + count[j]);
+        if (hit) {
+          const int lane = __ffsll((unsigned long long)hit) - 1;
+          *b = kPer * lane + j;
+          *t0 = (next - __builtin_amdgcn_readlane(before[j], lane)) * kTokens;
+        }
+      }
+      *s = seq_of(v, r, layer, *b);
+      *at_layer = layer;
+      if (any_sees(a, *s, *t0, min(*t0 + kTokens, s->n))) break;
+      const int t = *t0 + threadIdx.x;
+      if (a.out != a.mass && threadIdx.x < kTokens && t < s->n) a.out[s->at + t] = a.mass[s->at + t];
+    }
+    next += gridDim.x;
+    return true;
+  }
+};
+
+// A block takes tiles of 16*S tokens, and of a tile's G*S parts (16 tokens of a
+// group) each wave a quarter, whole groups first; the next part's K is on its way
+// while one is worked on, across tiles.  NB: the 16-row blocks of every sequence, which
+// stay in registers while the group does; 0: any number, read for each part.
+template <typename T, int D, int NB>
+constexpr int kResident = NB == 2 || (sizeof(T) == 4 && D == 128) ? 3 : 4;   // blocks of a CU
+template <typename T, int D, bool F4, int NB, int S>
+__global__ __launch_bounds__(kThreads, (kResident<T, D, NB>)) void mass_few(PagedView v, MassArgs a,
+                                                                          RowList r) {
+  using K = KRow<T, D, F4>;
+  constexpr int kTokens = 16 * S;
+  extern __shared__ float sums[];       // [2][G][kTokens]
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int pair = blockIdx.x / a.blocks, b = pair % r.n, layer = pair / r.n;
-  const Seq s = seq_of(v, a, r, layer, b);
-  if (s.T == 0) return;
-  const int64_t layer_at = (int64_t)layer * v.ls;
-  const size_t row_at = ((size_t)layer * a.n_rows + s.row0) * v.H;      // of q and lse
-  for (int tile = blockIdx.x % a.blocks; (int64_t)tile * 64 < s.n; tile += a.blocks) {
-    const int t0 = tile * 64;
-    if (!any_sees(a, s, t0, min(t0 + 64, s.n))) {
-      const int t = t0 + threadIdx.x;
-      if (threadIdx.x < 64 && t < s.n) s.out[t] = s.mass[t];
-      continue;
-    }
-    const auto load = [&](int it, K& k) {
-      const int item = wave * v.G + it, g = item >> 2;
-      const int t = min(t0 + 16 * (item & 3), (s.n - 1) & ~15);
-      const int page = s.table[t >> v.psh];
-      // where there is no page the products are of page 0's, and dropped
-      const char* block = v.k + layer_at + (int64_t)(is_page(v, page) ? page : 0) * v.ps + (int64_t)g * v.gs;
-      k.load(v, block, (t & (v.P - 1)) + l16, quad, v.ts);
-    };
-    K k;
-    load(0, k);
-    for (int it = 0; it < v.G; ++it) {
-      K next;
-      if (it + 1 < v.G) load(it + 1, next);
-      const int item = wave * v.G + it, g = item >> 2, t = t0 + 16 * (item & 3) + l16;
+  const int parts = v.G * S, per = (parts + 3) / 4;
+  const int p0 = wave * per, p1 = min(p0 + per, parts);       // of this wave
+  Tiles<kTokens> tiles(v, r);
+  Seq s;
+  int layer, b, t0;
+  bool more = tiles.take(v, a, r, &layer, &s, &b, &t0);
+  const auto load = [&](const Seq& q, int at_layer, int first, int part, K& k) {
+    const int g = part / S, t = min(first + 16 * (part % S), (q.n - 1) & ~15);
+    const int page = const_ints(q.table)[t >> v.psh];
+    // where there is no page the products are of page 0's, and dropped
+    k.load(v, v.k + (int64_t)at_layer * v.ls + (int64_t)(is_page(v, page) ? page : 0) * v.ps + (int64_t)g * v.gs,
+           (t & (v.P - 1)) + l16, quad, v.ts);
+  };
+  K k;
+  if (more && p0 < p1) load(s, layer, t0, p0, k);
+  Rows16<T, D, F4> rows[NB > 0 ? NB : 1];
+  int row_layer = -1, row_b = -1, row_g = -1;
+  for (int buf = 0; more; buf ^= 1) {
+    float* const mine = sums + buf * v.G * kTokens;
+    Seq s1;
+    int layer1, b1, t1;
+    const bool again = tiles.take(v, a, r, &layer1, &s1, &b1, &t1);
+    for (int part = p0; part < p1; ++part) {
+      const int g = part / S, t = t0 + 16 * (part % S) + l16;
+      if (NB > 0 && (g != row_g || b != row_b || layer != row_layer)) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) rows[i].load(v, a, s, layer, g, 16 * i);
+        row_g = g;
+        row_b = b;
+        row_layer = layer;
+      }
+      K k1;
+      if (part + 1 < p1) load(s, layer, t0, part + 1, k1);
+      else if (again) load(s1, layer1, t1, p0, k1);
       float sum = 0.f;
-      for (int r0 = 0; r0 < s.R; r0 += 16) {
-        const int mine = min(r0 + l16, s.R - 1), i = s.T == 1 ? 0 : mine / s.hpg;
-        const char* qr = a.q + (row_at + (size_t)i * v.H + g * s.hpg + (mine - i * s.hpg)) * D * sizeof(T);
-        f32x4 x{0.f, 0.f, 0.f, 0.f};
+      if constexpr (NB > 0) {
 #pragma unroll
-        for (int f = 0; f < K::NF; ++f)
-          x = F::mma(*reinterpret_cast<const frag*>(qr + K::q_byte(f, quad)), k.get(f), x);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = r0 + 4 * quad + e, at = min(row, s.R - 1), qi = s.T == 1 ? 0 : at / s.hpg;
-          const float lse = a.lse[row_at + (size_t)qi * v.H + g * s.hpg + (at - qi * s.hpg)];
-          const bool see = row < s.R && lse != -INFINITY && sees(a, s.first + qi, t);
-          const float w = __builtin_amdgcn_exp2f(fmaf(x[e], a.scale, -lse * kLog2e));
-          sum += see ? w : 0.f;
+        for (int i = 0; i < NB; ++i) sum += rows[i].weigh(a, k, t);
+      } else {
+        // (the rows that lie before the tile do not see it)
+        for (int r0 = max(t0 - s.first, 0) * s.hpg & ~15; r0 < s.R; r0 += 16) {
+          rows[0].load(v, a, s, layer, g, r0);
+          sum += rows[0].weigh(a, k, t);
         }
       }
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
-      if (quad == 0) sums[g * 64 + 16 * (item & 3) + l16] = sum;
-      k = next;
+      if (quad == 0) mine[g * kTokens + 16 * (part % S) + l16] = sum;
+      k = k1;
     }
     __syncthreads();
-    if (threadIdx.x < 64 && t0 + (int)threadIdx.x < s.n) {
+    const int t = t0 + threadIdx.x;
+    if (threadIdx.x < kTokens && t < s.n) {
       float add = 0.f;
-      for (int g = 0; g < v.G; ++g) add += sums[g * 64 + threadIdx.x];
-      store_mass(v, s, t0 + threadIdx.x, add);
+      for (int g = 0; g < v.G; ++g) add += mine[g * kTokens + threadIdx.x];
+      store_mass(v, a, s, t, add);
     }
-    __syncthreads();
+    s = s1;
+    layer = layer1;
+    b = b1;
+    t0 = t1;
+    more = again;
   }
 }
 
 // --------------------------------------------------------------- many rows
 
 constexpr int kTile = 256;         // tokens of a block, 64 to a wave
-constexpr int kStage = 64;         // rows in LDS at a time, twice
+constexpr int kStage = 64;         // rows of a stage
+constexpr int kRing = 3;           // stages in LDS: this one, the next, and one that is loading
 
 // Where 16-byte piece c of a row of Q lies in LDS: the lanes of a read, which
 // differ in the row, meet different banks.
@@ -230,18 +336,21 @@ __global__ __launch_bounds__(kThreads, 2) void mass_many(PagedView v, MassArgs a
   constexpr int NF = D / 16, NP = D / 8, kRow = D * 2;
   constexpr int kLoads = kStage * NP / kThreads;          // 16-byte pieces of a thread per stage
   constexpr int kLoadRows = kThreads / NP;
-  __shared__ __align__(1024) char qs[2][kStage * kRow];
-  __shared__ __align__(16) float ls[2][kStage];           // lse log2(e); infinite behind the last row
-  __shared__ __align__(16) int ps[2][kStage];             // the rows' positions; -1: sees nothing
-  __shared__ int odd[2][2];                               // of 32 rows: some see nothing
+  // (three arrays, so that a read of one need not wait for loads into another)
+  __shared__ __align__(1024) char q0[kStage * kRow], q1[kStage * kRow], q2[kStage * kRow];
+  __shared__ __align__(16) float ls[kRing][kStage];       // lse log2(e); infinite behind the last row
+  __shared__ __align__(16) int ps[kRing][kStage];         // the rows' positions; -1: sees nothing
+  __shared__ int span[kRing][2][2];                       // the least (-1: some see nothing) and largest of 32
 
   const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int split = blockIdx.x % a.n_split, at = blockIdx.x / a.n_split;
   const int pair = at / a.blocks, b = pair % r.n, layer = pair / r.n;
-  const Seq s = seq_of(v, a, r, layer, b);
+  const Seq s = seq_of(v, r, layer, b);
   if (s.T == 0) return;
   const size_t row_at = ((size_t)layer * a.n_rows + s.row0) * v.H;
+  // x / hpg is the upper half of x * per_head for x < 2^20 (hpg is under 2^12)
+  const uint32_t per_head = (uint32_t)(((1ull << 32) + s.hpg - 1) / s.hpg);
 
   for (int tile = at % a.blocks; (int64_t)tile * kTile < s.n; tile += a.blocks) {
     // tiles behind the bound that the splits' sums were sized by are not split
@@ -258,7 +367,7 @@ __global__ __launch_bounds__(kThreads, 2) void mass_many(PagedView v, MassArgs a
     int64_t w0 = shared_tile ? all * split / a.n_split : 0;
     const int64_t w1 = shared_tile ? all * (split + 1) / a.n_split : all;
 
-    float sum[2] = {0.f, 0.f};
+    float sum[2][2] = {};
     while (w0 < w1) {
       const int g = (int)(w0 / (p1 - p0));
       const int from = p0 + (int)(w0 - (int64_t)g * (p1 - p0));
@@ -288,112 +397,175 @@ __global__ __launch_bounds__(kThreads, 2) void mass_many(PagedView v, MassArgs a
           for (int f = 0; f < NF; ++f) kf[h][f] = *reinterpret_cast<const bf16x8*>(row + 16 * f);
         }
       }
-      // rows 32*from.. in stages of 64; the thread's rows of a stage are kLoadRows apart
+      // Rows 32*from.. in stages of 64, asked for in order: query token i0 and head h0
+      // are the stage's first row, and row x behind it is head (h0 + x) % hpg of token
+      // i0 + (h0 + x) / hpg; rows behind the last repeat it.  A thread's pieces are of
+      // rows kLoadRows apart, whose places in LDS are permuted alike
       const int piece = threadIdx.x % NP, sub = threadIdx.x / NP;
-      const auto stage = [&](int first, int buf) {
+      const size_t group_at = row_at + g * s.hpg;
+      const uint32_t at_piece = (piece ^ q_swizzle<D>(sub)) * 16;
+      static_assert(q_swizzle<D>(kLoadRows) == 0, "whole turns of the swizzle");
+      int first = 32 * from, i0 = first / s.hpg, h0 = first - i0 * s.hpg;
+      const int ahead_i = kStage / s.hpg, ahead_h = kStage - ahead_i * s.hpg;
+      // of wave 0's lanes: a row's log-sum, read a stage ahead, and its query token
+      int lrow = 32 * from + lane, li = lrow / s.hpg, lhead = lrow - li * s.hpg;
+      const auto log_sum = [&]() {
+        return lrow < s.R ? a.lse[group_at + (size_t)li * v.H + lhead] : -INFINITY;
+      };
+      float lse = wave == 0 ? log_sum() : 0.f;
+      const auto stage = [&](char* to, int buf) {
+        // (before the loads into LDS: what waits for the log-sums waits for all loads before)
+        if (wave == 0) {
+          // (also for the rows behind the last)
+          const bool none = lse == -INFINITY;
+          const float l = none ? INFINITY : lse * kLog2e;
+          const int p = none ? -1 : s.first + li;
+          ls[buf][lane] = l;
+          ps[buf][lane] = p;
+          // positions rise with the rows: the first and the last of each 32, or -1
+          // where one sees nothing
+          const uint64_t dead = __ballot(p < 0);
+          if (l32 == 0) span[buf][half][0] = (uint32_t)(dead >> (32 * half)) ? -1 : p;
+          if (l32 == 31) span[buf][half][1] = p;
+          lrow += kStage;
+          li += ahead_i;
+          lhead += ahead_h;
+          if (lhead >= s.hpg) {
+            lhead -= s.hpg;
+            ++li;
+          }
+          lse = log_sum();
+        }
+        const char* const at = a.q + (group_at + (size_t)i0 * v.H) * kRow;
+        const int last = h0 + s.R - 1 - first;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-          const int in_stage = sub + j * kLoadRows, row = min(first + in_stage, s.R - 1), i = row / s.hpg;
-          const char* qr = a.q + (row_at + (size_t)i * v.H + g * s.hpg + (row - i * s.hpg)) * kRow;
-          __builtin_amdgcn_global_load_lds(
-              (const __attribute__((address_space(1))) void*)(qr + (piece ^ q_swizzle<D>(in_stage)) * 16),
-              (__attribute__((address_space(3))) void*)(qs[buf] + (wave * 64 / NP + j * kLoadRows) * kRow),
-              16, 0, 0);
+          const uint32_t x = min(h0 + sub + j * kLoadRows, last), i = s.hpg == 1 ? x : __umulhi(x, per_head);
+          const uint32_t off = (i * (uint32_t)(v.H - s.hpg) + x) * kRow + at_piece;
+          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(at + off),
+                                           (__attribute__((address_space(3))) void*)(to + (wave * 64 / NP + j * kLoadRows) * kRow),
+                                           16, 0, 0);
         }
-        if (threadIdx.x < kStage) {
-          const int row = first + threadIdx.x, i = min(row, s.R - 1) / s.hpg;
-          float l = INFINITY;
-          int p = -1;
-          if (row < s.R) {
-            const float lse = a.lse[row_at + (size_t)i * v.H + g * s.hpg + (row - i * s.hpg)];
-            if (lse != -INFINITY) {
-              l = lse * kLog2e;
-              p = s.first + i;
-            }
-          }
-          ls[buf][threadIdx.x] = l;
-          ps[buf][threadIdx.x] = p;
-          const uint64_t dead = __ballot(p < 0);
-          if (threadIdx.x < 2) odd[buf][threadIdx.x] = (uint32_t)(dead >> (32 * threadIdx.x)) != 0;
+        first += kStage;
+        i0 += ahead_i;
+        h0 += ahead_h;
+        if (h0 >= s.hpg) {
+          h0 -= s.hpg;
+          ++i0;
         }
       };
-      const int rows = to - from;           // of 32 each
-      int buf = 0;
-      __syncthreads();                      // the rows before are done with
-      stage(32 * from, 0);
-      for (int j = 0; j < rows; j += 2, buf ^= 1) {
-        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-        __syncthreads();
-        if (j + 2 < rows) stage(32 * (from + j + 2), buf ^ 1);
-        const int tw = t0 + 64 * wave;        // the wave's first token
+      // A step takes the weights of one 32-row product while the next runs on the
+      // matrix units: x holds product j, y becomes product j + 1
+      const int rows = to - from;           // products
+      const int tw = t0 + 64 * wave, te = min(tw + 64, s.n);        // the wave's tokens
+      using Product = f32x16[2];
+      Product x, y;
+      const auto q_frag = [&](const char* qs, int u, int f) {
+        const int row = 32 * u + l32;
+        return *reinterpret_cast<const bf16x8*>(qs + row * kRow + (((half * NP / 2 + f) ^ q_swizzle<D>(row)) * 16));
+      };
+      // the weights of x, half u of stage `buf`, beside the product y of the rows at
+      // qn, half un
+      const auto step = [&](Product& x, int buf, int u, Product& y, const char* qn, int un) {
+        f32x4 l4[4];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          if (j + u >= rows) break;
-          f32x16 x[2];
+        for (int e = 0; e < 4; ++e) l4[e] = *reinterpret_cast<const f32x4*>(&ls[buf][32 * u + 8 * e + 4 * half]);
+        // unless all rows see all tokens of the wave that there are
+        const int p_first = __builtin_amdgcn_readfirstlane(span[buf][u][0]);
+        const int p_last = __builtin_amdgcn_readfirstlane(span[buf][u][1]);
+        if (te - 1 > p_first || !(tw > p_last - a.window || te <= a.sinks)) {
 #pragma unroll
-          for (int f = 0; f < NF; ++f) {
-            const int row = 32 * u + l32;
-            const bf16x8 qf = *reinterpret_cast<const bf16x8*>(
-                qs[buf] + row * kRow + (((half * NP / 2 + f) ^ q_swizzle<D>(row)) * 16));
+          for (int e = 0; e < 16; ++e) {
+            const int p = ps[buf][32 * u + 8 * (e >> 2) + 4 * half + (e & 3)];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-              x[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[h][f], f ? x[h] : f32x16{}, 0, 0, 0);
-          }
-          f32x4 l4[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            l4[e] = *reinterpret_cast<const f32x4*>(&ls[buf][32 * u + 8 * e + 4 * half]);
-          // all rows see all tokens of the wave that there are
-          const int r_first = 32 * (from + j + u), i_first = r_first / s.hpg;
-          const int i_last = min(r_first + 31, s.R - 1) / s.hpg;
-          const int te = min(tw + 64, s.n);
-          const bool whole = !odd[buf][u] && te - 1 <= s.first + i_first &&
-                             (tw > s.first + i_last - a.window || te <= a.sinks);
-          if (whole) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int e = 0; e < 16; ++e)
-                sum[h] += __builtin_amdgcn_exp2f(fmaf(x[h][e], a.scale, -l4[e >> 2][e & 3]));
-          } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int p = ps[buf][32 * u + 8 * (e >> 2) + 4 * half + (e & 3)];
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const float w = __builtin_amdgcn_exp2f(fmaf(x[h][e], a.scale, -l4[e >> 2][e & 3]));
-                sum[h] += sees(a, p, tw + 32 * h + l32) ? w : 0.f;
-              }
-            }
+            for (int h = 0; h < 2; ++h) x[h][e] = sees(a, p, tw + 32 * h + l32) ? x[h][e] : -INFINITY;
           }
         }
+        constexpr int kShare = 32 / NF;
+        bf16x8 qf[NF];
+        qf[0] = q_frag(qn, un, 0);
+        qf[1] = q_frag(qn, un, 1);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            y[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[f], kf[h][f], f ? y[h] : f32x16{}, 0, 0, 0);
+          if (f + 2 < NF) qf[f + 2] = q_frag(qn, un, f + 2);
+#pragma unroll
+          for (int i = 0; i < kShare; ++i) {
+            const int w = kShare * f + i, e = w >> 1, h = w & 1;
+            sum[h][e & 1] += __builtin_amdgcn_exp2f(fmaf(x[h][e], a.scale, -l4[e >> 2][e & 3]));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      const auto landed = [&]() {
+        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+        __syncthreads();
+      };
+      __syncthreads();                        // the rows before are done with
+      stage(q0, 0);
+      if (rows > 2) stage(q1, 1);
+      landed();
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          x[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q_frag(q0, 0, f), kf[h][f], f ? x[h] : f32x16{}, 0, 0, 0);
+      // stage products j and j + 1; behind the last come products of whatever LDS
+      // holds, and nobody reads them
+      const auto two = [&](int j, const char* q, int buf, const char* qn, char* free, int free_buf) {
+        // the next stage has landed, and every wave is done with the one before
+        if (j) landed();
+        if (j + 4 < rows) stage(free, free_buf);
+        step(x, buf, 0, y, q, 1);
+        if (j + 1 < rows) step(y, buf, 1, x, qn, 0);
+      };
+      for (int j = 0; j < rows; j += 6) {
+        two(j, q0, 0, q1, q2, 2);
+        if (j + 2 < rows) two(j + 2, q1, 1, q2, q0, 0);
+        if (j + 4 < rows) two(j + 4, q2, 2, q0, q1, 1);
       }
     }
     // the two halves' rows; lane l32 of half h writes token 32 h + l32
 #pragma unroll
-    for (int h = 0; h < 2; ++h) sum[h] += __shfl_xor(sum[h], 32);
+    for (int h = 0; h < 2; ++h) {
+      sum[h][0] += sum[h][1];
+      sum[h][0] += __shfl_xor(sum[h][0], 32);
+    }
     const int t = t0 + 64 * wave + lane;
-    const float add = half ? sum[1] : sum[0];
+    const float add = half ? sum[1][0] : sum[0][0];
     if (shared_tile)
       a.part[((size_t)pair * a.n_split + split) * a.tiles * kTile + t] = add;
     else if (t < s.n)
-      store_mass(v, s, t, add);
+      store_mass(v, a, s, t, add);
   }
 }
 
 // The splits' sums of the tokens within the bound, one after the other.
 __global__ __launch_bounds__(kThreads) void mass_join(PagedView v, MassArgs a, RowList r) {
   const int b = blockIdx.x % r.n, layer = blockIdx.x / r.n;
-  const Seq s = seq_of(v, a, r, layer, b);
+  const Seq s = seq_of(v, r, layer, b);
   if (s.T == 0) return;
   const int bound = a.tiles * kTile;
   const float* part = a.part + (size_t)blockIdx.x * a.n_split * bound;
   for (int t = blockIdx.y * kThreads + threadIdx.x; t < min(s.n, bound); t += gridDim.y * kThreads) {
-    float add = 0.f;
-    for (int i = 0; i < a.n_split; ++i) add += part[(size_t)i * bound + t];
-    store_mass(v, s, t, add);
+    float add[4] = {};
+    for (int i = 0; i < a.n_split; i += 4) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (i + j < a.n_split) add[j] += part[(size_t)(i + j) * bound + t];
+    }
+    store_mass(v, a, s, t, (add[0] + add[1]) + (add[2] + add[3]));
   }
 }
+
+template <int I>
+using Int = std::integral_constant<int, I>;
+template <typename T>
+struct Type {
+  using type = T;
+};
 
 }  // namespace
 
@@ -412,9 +584,9 @@ int launch_mass_add(const PagedView& v, const MassCall& c, void* stream) {
   a.tiles = c.s.tiles;
   a.n_split = c.s.n_split;
   a.scale = kLog2e / sqrtf((float)v.d);
-  const unsigned pairs = (unsigned)(v.n_layers * c.r.n);
-  const unsigned blocks = pairs * c.s.blocks * c.s.n_split;
   if (c.s.many) {
+    const unsigned pairs = (unsigned)(v.n_layers * c.r.n);
+    const unsigned blocks = pairs * c.s.blocks * c.s.n_split;
     const auto go = [&](auto kernel) { kernel<<<blocks, kThreads, 0, st>>>(v, a, c.r); };
     if (v.d == 128) v.fp4 ? go(mass_many<128, true>) : go(mass_many<128, false>);
     else v.fp4 ? go(mass_many<64, true>) : go(mass_many<64, false>);
@@ -424,11 +596,27 @@ int launch_mass_add(const PagedView& v, const MassCall& c, void* stream) {
     }
     return (int)hipGetLastError();
   }
-  const size_t lds = (size_t)v.G * 64 * sizeof(float);
-  const auto go = [&](auto kernel) { kernel<<<blocks, kThreads, lds, st>>>(v, a, c.r); };
-  if (v.fp4) v.d == 128 ? go(mass_few<__bf16, 128, true>) : go(mass_few<__bf16, 64, true>);
-  else if (v.esz == 2) v.d == 128 ? go(mass_few<__bf16, 128, false>) : go(mass_few<__bf16, 64, false>);
-  else v.d == 128 ? go(mass_few<float, 128, false>) : go(mass_few<float, 64, false>);
+  const size_t lds = (size_t)2 * v.G * c.s.tile * sizeof(float);
+  const auto by_tile = [&](auto t, auto d, auto f4, auto nb) {
+    using T = typename decltype(t)::type;
+    constexpr int D = decltype(d)::value, NB = decltype(nb)::value;
+    constexpr bool F4 = decltype(f4)::value;
+    const unsigned blocks = (unsigned)std::min<int64_t>(c.s.blocks, 256 * kResident<T, D, NB>);
+    const auto go = [&](auto kernel) { kernel<<<blocks, kThreads, lds, st>>>(v, a, c.r); };
+    c.s.tile == 64 ? go(mass_few<T, D, F4, NB, 4>) : go(mass_few<T, D, F4, NB, 1>);
+  };
+  const auto by_rows = [&](auto t, auto d, auto f4) {
+    using T = typename decltype(t)::type;
+    if (c.s.row_blocks == 1) by_tile(t, d, f4, Int<1>{});
+    else if constexpr (sizeof(T) == 2) by_tile(t, d, f4, Int<2>{});
+    else by_tile(t, d, f4, Int<0>{});
+  };
+  const auto by_type = [&](auto d) {
+    if (v.fp4) by_rows(Type<__bf16>{}, d, std::true_type{});
+    else if (v.esz == 2) by_rows(Type<__bf16>{}, d, std::false_type{});
+    else by_rows(Type<float>{}, d, std::false_type{});
+  };
+  v.d == 128 ? by_type(Int<128>{}) : by_type(Int<64>{});
   return (int)hipGetLastError();
 }
 
