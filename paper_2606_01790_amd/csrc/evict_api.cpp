@@ -38,8 +38,9 @@ starkv_status mass_shape(const PagedView& v, const int32_t* rows, int n, int32_t
   s->n_split = 1;
   s->ws_bytes = 0;
   if (!s->many) {
-    // small tiles where large ones are too few for the card
-    s->tile = pairs * ((len + 63) / 64) >= 512 ? 64 : 16;
+    // tiles of four parts, or of one where those are too few for the card
+    const int part = v.fp4 ? 32 : 16;
+    s->tile = pairs * ((len + 4 * part - 1) / (4 * part)) >= 512 ? 4 * part : part;
     s->tiles = (int)((len + s->tile - 1) / s->tile);
     s->blocks = (int)std::min<int64_t>(pairs * s->tiles, 1 << 20);   // (the launch takes what the card holds)
     return STARKV_OK;

@@ -43,21 +43,25 @@ struct MassArgs {
 struct Seq {
   int n, T, first;          // length, query tokens, position of the first (may be negative)
   int row0, hpg, R;         // its first row of the call; heads, and rows, of a group
-  const int32_t* table;
-  size_t at;                // its first mass
+  int slot, layer;
 };
 __device__ inline Seq seq_of(const PagedView& v, const RowList& r, int layer, int b) {
   Seq s;
-  const int slot = r.slot[b];
-  s.n = min(max(const_ints(v.len)[slot], 0), v.cap);
+  s.slot = r.slot[b];
+  s.layer = layer;
+  s.n = min(max(const_ints(v.len)[s.slot], 0), v.cap);
   s.row0 = r.row0[b];
   s.T = r.row0[b + 1] - s.row0;
   s.first = s.n - s.T;
   s.hpg = v.H / v.G;
   s.R = s.T * s.hpg;
-  s.table = v.table + (size_t)slot * v.max_pages;
-  s.at = ((size_t)layer * v.n_slots + slot) * v.cap;
   return s;
+}
+__device__ inline size_t first_mass(const PagedView& v, const Seq& s) {
+  return ((size_t)s.layer * v.n_slots + s.slot) * v.cap;
+}
+__device__ inline const int32_t* table_of(const PagedView& v, const Seq& s) {
+  return v.table + (size_t)s.slot * v.max_pages;
 }
 __device__ inline bool is_page(const PagedView& v, int p) { return p >= 0 && p < v.n_pages; }
 
@@ -65,8 +69,9 @@ __device__ inline bool is_page(const PagedView& v, int p) { return p >= 0 && p <
 // whatever was computed in its place).
 __device__ inline void store_mass(const PagedView& v, const MassArgs& a, const Seq& s, int t,
                                   float add) {
-  const float old = t < s.first ? a.mass[s.at + t] : 0.f;
-  a.out[s.at + t] = is_page(v, s.table[t >> v.psh]) ? old + add : old;
+  const size_t at = first_mass(v, s) + t;
+  const float old = t < s.first ? a.mass[at] : 0.f;
+  a.out[at] = is_page(v, table_of(v, s)[t >> v.psh]) ? old + add : old;
 }
 // Whether any row sees any of the tokens [t0, t1).
 __device__ inline bool any_sees(const MassArgs& a, const Seq& s, int t0, int t1) {
@@ -100,6 +105,14 @@ struct Frag<float> {
     return c;
   }
 };
+
+// The sum over the four lanes of the same l16, in all of them.
+__device__ inline float quads_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
 
 // Four elements' pairs of a 4-bit word, times the scale, exactly.
 __device__ inline bf16x8 from_fp4(uint32_t w, float s) {
@@ -150,10 +163,9 @@ struct Rows16 {
   typename Frag<T>::type q[K::NF];
   float l[4];
   int p[4];
-  __device__ inline void load(const PagedView& v, const MassArgs& a, const Seq& s, int layer, int g,
-                              int r0) {
+  __device__ inline void load(const PagedView& v, const MassArgs& a, const Seq& s, int g, int r0) {
     const int l16 = threadIdx.x & 15, quad = threadIdx.x >> 4 & 3;
-    const size_t at = ((size_t)layer * a.n_rows + s.row0) * v.H + g * s.hpg;
+    const size_t at = ((size_t)s.layer * a.n_rows + s.row0) * v.H + g * s.hpg;
     const int mine = min(r0 + l16, s.R - 1), i = mine / s.hpg;
     const char* qr = a.q + (at + (size_t)i * v.H + (mine - i * s.hpg)) * D * sizeof(T);
 #pragma unroll
@@ -167,18 +179,23 @@ struct Rows16 {
       p[e] = row < s.R && lse != -INFINITY ? s.first + qi : -1;
     }
   }
-  // The lane's rows' weights of token t, whose part of K the lane holds.
-  __device__ inline float weigh(const MassArgs& a, const K& k, int t) const {
+  // The lane's rows' weights of token t, whose part of K the lane holds.  `whole`:
+  // every row but those that see nothing (p < 0) sees it.
+  __device__ inline float weigh(const MassArgs& a, const K& k, int t, bool whole) const {
     f32x4 x{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int f = 0; f < K::NF; ++f) x = Frag<T>::mma(q[f], k.get(f), x);
-    float sum = 0.f;
+    float w[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float w = __builtin_amdgcn_exp2f(fmaf(x[e], a.scale, -l[e]));
-      sum += sees(a, p[e], t) ? w : 0.f;
+    for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_exp2f(fmaf(x[e], a.scale, -l[e]));
+    if (whole) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = __uint_as_float(__float_as_uint(w[e]) & ~(p[e] >> 31));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = sees(a, p[e], t) ? w[e] : 0.f;
     }
-    return sum;
+    return (w[0] + w[1]) + (w[2] + w[3]);
   }
 };
 
@@ -209,112 +226,136 @@ struct Tiles {
 #pragma unroll
     for (int j = 1; j < kPer; ++j) before[j] = before[j - 1] + count[j - 1];
   }
-  // The block's next tile that rows see, into b and t0; the others keep their
-  // masses.  False when there is none.
-  __device__ inline bool take(const PagedView& v, const MassArgs& a, const RowList& r, int* at_layer,
-                              Seq* s, int* b, int* t0) {
+  // The block's next tile that rows see, of sequence s from token t0 on; the others
+  // keep their masses.  False when there is none.
+  __device__ inline bool take(const PagedView& v, const MassArgs& a, const RowList& r, Seq* s,
+                              int* t0) {
     if (all == 0) return false;
     for (;; next += gridDim.x) {
       while (next >= all) {
         next -= all;
         if (++layer >= v.n_layers) return false;
       }
+      int b = 0;
 #pragma unroll
       for (int j = 0; j < kPer; ++j) {
         const uint64_t hit = __ballot(before[j] <= next && next < before[j] + count[j]);
         if (hit) {
           const int lane = __ffsll((unsigned long long)hit) - 1;
-          *b = kPer * lane + j;
+          b = kPer * lane + j;
           *t0 = (next - __builtin_amdgcn_readlane(before[j], lane)) * kTokens;
         }
       }
-      *s = seq_of(v, r, layer, *b);
-      *at_layer = layer;
+      *s = seq_of(v, r, layer, b);
       if (any_sees(a, *s, *t0, min(*t0 + kTokens, s->n))) break;
       const int t = *t0 + threadIdx.x;
-      if (a.out != a.mass && threadIdx.x < kTokens && t < s->n) a.out[s->at + t] = a.mass[s->at + t];
+      if (a.out != a.mass && threadIdx.x < kTokens && t < s->n) a.out[first_mass(v, *s) + t] = a.mass[first_mass(v, *s) + t];
     }
     next += gridDim.x;
     return true;
   }
 };
 
-// A block takes tiles of 16*S tokens, and of a tile's G*S parts (16 tokens of a
-// group) each wave a quarter, whole groups first; the next part's K is on its way
-// while one is worked on, across tiles.  NB: the 16-row blocks of every sequence, which
-// stay in registers while the group does; 0: any number, read for each part.
+// A block takes tiles of S parts of a group (four, or one where those tiles are too few;
+// a part is 16 tokens, 32 in 4 bits, whose rows are shorter), and of all groups' parts
+// each wave a quarter, whole groups first.  The next part's K is on its way while one is worked
+// on, across tiles.  NB: the 16-row blocks of every sequence, which stay in registers
+// while the group does; 0: any number, read for each part.
 template <typename T, int D, int NB>
-constexpr int kResident = NB == 2 || (sizeof(T) == 4 && D == 128) ? 3 : 4;   // blocks of a CU
+constexpr int kResident = sizeof(T) == 4 && D == 128 ? (NB == 2 ? 2 : 3) : NB == 1 ? 5 : 4;   // blocks of a CU
+template <bool F4>
+constexpr int kPart = F4 ? 32 : 16;
 template <typename T, int D, bool F4, int NB, int S>
 __global__ __launch_bounds__(kThreads, (kResident<T, D, NB>)) void mass_few(PagedView v, MassArgs a,
                                                                           RowList r) {
-  using K = KRow<T, D, F4>;
-  constexpr int kTokens = 16 * S;
+  constexpr int kTokens = S * kPart<F4>, kHalves = kPart<F4> / 16;
+  struct K {
+    KRow<T, D, F4> half[kHalves];
+  };
   extern __shared__ float sums[];       // [2][G][kTokens]
   const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int parts = v.G * S, per = (parts + 3) / 4;
   const int p0 = wave * per, p1 = min(p0 + per, parts);       // of this wave
   Tiles<kTokens> tiles(v, r);
-  Seq s;
-  int layer, b, t0;
-  bool more = tiles.take(v, a, r, &layer, &s, &b, &t0);
-  const auto load = [&](const Seq& q, int at_layer, int first, int part, K& k) {
-    const int g = part / S, t = min(first + 16 * (part % S), (q.n - 1) & ~15);
-    const int page = const_ints(q.table)[t >> v.psh];
-    // where there is no page the products are of page 0's, and dropped
-    k.load(v, v.k + (int64_t)at_layer * v.ls + (int64_t)(is_page(v, page) ? page : 0) * v.ps + (int64_t)g * v.gs,
-           (t & (v.P - 1)) + l16, quad, v.ts);
-  };
-  K k;
-  if (more && p0 < p1) load(s, layer, t0, p0, k);
-  Rows16<T, D, F4> rows[NB > 0 ? NB : 1];
-  int row_layer = -1, row_b = -1, row_g = -1;
-  for (int buf = 0; more; buf ^= 1) {
-    float* const mine = sums + buf * v.G * kTokens;
-    Seq s1;
-    int layer1, b1, t1;
-    const bool again = tiles.take(v, a, r, &layer1, &s1, &b1, &t1);
-    for (int part = p0; part < p1; ++part) {
-      const int g = part / S, t = t0 + 16 * (part % S) + l16;
-      if (NB > 0 && (g != row_g || b != row_b || layer != row_layer)) {
+  Seq s, s1;                            // this tile and the next
+  int t0, t1, part = p0, buf = 0;
+  bool again = false, whole = false;
+  const auto load = [&](const Seq& q, int first, int p, K& k) {
+    const int g = p / S;
 #pragma unroll
-        for (int i = 0; i < NB; ++i) rows[i].load(v, a, s, layer, g, 16 * i);
-        row_g = g;
-        row_b = b;
-        row_layer = layer;
-      }
-      K k1;
-      if (part + 1 < p1) load(s, layer, t0, part + 1, k1);
-      else if (again) load(s1, layer1, t1, p0, k1);
-      float sum = 0.f;
-      if constexpr (NB > 0) {
-#pragma unroll
-        for (int i = 0; i < NB; ++i) sum += rows[i].weigh(a, k, t);
-      } else {
-        // (the rows that lie before the tile do not see it)
-        for (int r0 = max(t0 - s.first, 0) * s.hpg & ~15; r0 < s.R; r0 += 16) {
-          rows[0].load(v, a, s, layer, g, r0);
-          sum += rows[0].weigh(a, k, t);
-        }
-      }
-      sum += __shfl_xor(sum, 16);
-      sum += __shfl_xor(sum, 32);
-      if (quad == 0) mine[g * kTokens + 16 * (part % S) + l16] = sum;
-      k = k1;
+    for (int h = 0; h < kHalves; ++h) {
+      const int t = min(first + kPart<F4> * (p % S) + 16 * h, (q.n - 1) & ~15);
+      const int page = const_ints(table_of(v, q))[t >> v.psh];
+      // where there is no page the products are of page 0's, and dropped
+      k.half[h].load(v, v.k + (int64_t)q.layer * v.ls + (int64_t)(is_page(v, page) ? page : 0) * v.ps +
+                            (int64_t)g * v.gs,
+                     (t & (v.P - 1)) + l16, quad, v.ts);
     }
+  };
+  const auto begin = [&]() {
+    const int te = min(t0 + kTokens, s.n);
+    whole = te - 1 <= s.first && (t0 > s.n - 1 - a.window || te <= a.sinks);
+  };
+  Rows16<T, D, F4> rows[NB > 0 ? NB : 1];
+  int row_layer = -1, row_slot = -1, row_g = -1;
+  // the wave's next part, K of which is in `k`; K of the one behind it comes into
+  // `ahead`.  False behind the last
+  const auto step = [&](K& k, K& ahead) {
+    const int g = part / S;
+    const bool last = part + 1 >= p1;
+    if (NB > 0 && part < p1 && (g != row_g || s.slot != row_slot || s.layer != row_layer)) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) rows[i].load(v, a, s, g, 16 * i);
+      __builtin_amdgcn_s_waitcnt(0x0F70);   // here, and not behind the next K below
+      row_g = g;
+      row_slot = s.slot;
+      row_layer = s.layer;
+    }
+    if (last) again = tiles.take(v, a, r, &s1, &t1);
+    if (!last) load(s, t0, part + 1, ahead);
+    else if (again && p0 < p1) load(s1, t1, p0, ahead);
+    float* const mine = sums + buf * v.G * kTokens;
+    if (part < p1) {
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        const int in_tile = kPart<F4> * (part % S) + 16 * h + l16, t = t0 + in_tile;
+        float sum = 0.f;
+        if constexpr (NB > 0) {
+#pragma unroll
+          for (int i = 0; i < NB; ++i) sum += rows[i].weigh(a, k.half[h], t, whole);
+        } else {
+          // (the rows that lie before the tile do not see it)
+          for (int r0 = max(t0 - s.first, 0) * s.hpg & ~15; r0 < s.R; r0 += 16) {
+            rows[0].load(v, a, s, g, r0);
+            sum += rows[0].weigh(a, k.half[h], t, whole);
+          }
+        }
+        sum = quads_sum(sum);
+        if (quad == 0) mine[g * kTokens + in_tile] = sum;
+      }
+    }
+    ++part;
+    if (!last) return true;
     __syncthreads();
     const int t = t0 + threadIdx.x;
     if (threadIdx.x < kTokens && t < s.n) {
       float add = 0.f;
-      for (int g = 0; g < v.G; ++g) add += mine[g * kTokens + threadIdx.x];
+      for (int i = 0; i < v.G; ++i) add += mine[i * kTokens + threadIdx.x];
       store_mass(v, a, s, t, add);
     }
     s = s1;
-    layer = layer1;
-    b = b1;
     t0 = t1;
-    more = again;
+    part = p0;
+    buf ^= 1;
+    begin();
+    return again;
+  };
+  if (!tiles.take(v, a, r, &s, &t0)) return;
+  begin();
+  K ka, kb;
+  if (p0 < p1) load(s, t0, p0, ka);
+  while (step(ka, kb) && step(kb, ka)) {
   }
 }
 
@@ -378,7 +419,7 @@ __global__ __launch_bounds__(kThreads, 2) void mass_many(PagedView v, MassArgs a
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int t = min(t0 + 64 * wave + 32 * h + l32, s.n - 1);
-        const int page = s.table[t >> v.psh], in_page = t & (v.P - 1);
+        const int page = table_of(v, s)[t >> v.psh], in_page = t & (v.P - 1);
         const char* block = v.k + (int64_t)layer * v.ls + (int64_t)(is_page(v, page) ? page : 0) * v.ps +
                             (int64_t)g * v.gs;
         if constexpr (F4) {
@@ -603,13 +644,13 @@ int launch_mass_add(const PagedView& v, const MassCall& c, void* stream) {
     constexpr bool F4 = decltype(f4)::value;
     const unsigned blocks = (unsigned)std::min<int64_t>(c.s.blocks, 256 * kResident<T, D, NB>);
     const auto go = [&](auto kernel) { kernel<<<blocks, kThreads, lds, st>>>(v, a, c.r); };
-    c.s.tile == 64 ? go(mass_few<T, D, F4, NB, 4>) : go(mass_few<T, D, F4, NB, 1>);
+    c.s.tile == kPart<F4> ? go(mass_few<T, D, F4, NB, 1>) : go(mass_few<T, D, F4, NB, 4>);
   };
   const auto by_rows = [&](auto t, auto d, auto f4) {
     using T = typename decltype(t)::type;
     if (c.s.row_blocks == 1) by_tile(t, d, f4, Int<1>{});
-    else if constexpr (sizeof(T) == 2) by_tile(t, d, f4, Int<2>{});
-    else by_tile(t, d, f4, Int<0>{});
+    else if (sizeof(T) == 2 || c.s.row_blocks == 2) by_tile(t, d, f4, Int<2>{});
+    else if constexpr (sizeof(T) == 4) by_tile(t, d, f4, Int<0>{});
   };
   const auto by_type = [&](auto d) {
     if (v.fp4) by_rows(Type<__bf16>{}, d, std::true_type{});
