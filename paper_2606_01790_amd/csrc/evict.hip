@@ -4,10 +4,11 @@
 //
 // One block of 16 waves works on a (layer, sequence).  The masses become 32-bit
 // keys in the order of the numbers, a wave keeps a range of tokens' keys in its
-// registers, and the largest threshold that K keys reach is found bit by bit: the
-// lanes of a wave are counted by a ballot, so a round is a compare and a count of
-// bits per 64 keys and one barrier, whatever the distribution of the masses.  It
-// ends early where the count is met.
+// registers, and the largest threshold that K keys reach is found bit by bit: a round
+// is two instructions per 64 keys, a sum and one barrier, whatever the distribution of
+// the masses.  What a round costs is what its 16 waves issue, so once few keys agree with the threshold so
+// far they go to one wave, which ends the search alone.  It ends early where the count
+// is met.
 #include <algorithm>
 
 #include "device_common.h"
@@ -42,112 +43,184 @@ __device__ inline float* mass_row(const PagedView& v, float* mass, int layer, in
   return mass + ((size_t)layer * v.n_slots + slot) * v.cap;
 }
 
-// Sinks above all, then NaN, then the masses; 0: not to be kept.
-constexpr uint32_t kSink = ~0u, kNan = ~0u - 1;
-__device__ inline uint32_t key_of(const PagedView& v, const int32_t* table, const float* mass,
-                                  int t, int span, int sinks) {
-  if (t >= span) return 0;
-  const int page = table[t >> v.psh];
-  if (page < 0 || page >= v.n_pages) return 0;
-  if (t < sinks) return kSink;
-  const float m = mass[t];
-  return m != m ? kNan : fkey(m + 0.f);      // (-0 counts as 0)
+// The sum over the 16 lanes of a row, in all of them.
+__device__ inline int row_sum(int x) {
+  x += __builtin_amdgcn_mov_dpp(x, 0x128, 0xF, 0xF, true);     // the row turned by 8, 4, 2, 1
+  x += __builtin_amdgcn_mov_dpp(x, 0x124, 0xF, 0xF, true);
+  x += __builtin_amdgcn_mov_dpp(x, 0x122, 0xF, 0xF, true);
+  return x + __builtin_amdgcn_mov_dpp(x, 0x121, 0xF, 0xF, true);
+}
+// The sum over the wave.
+__device__ inline int wave_sum(int x) {
+  x = row_sum(x);
+  return __builtin_amdgcn_readlane(x, 0) + __builtin_amdgcn_readlane(x, 16) + __builtin_amdgcn_readlane(x, 32) +
+         __builtin_amdgcn_readlane(x, 48);
 }
 
-// The keys of a wave's tokens [first, first + 64 * count): in N registers a lane,
-// or (N = 0) read again each time.
+// Sinks above all, then NaN, then the masses; 0: not to be kept.
+constexpr uint32_t kSink = ~0u, kNan = ~0u - 1;
+__device__ inline uint32_t key_of(const PagedView& v, int page, float m, int t, int span, int sinks) {
+  if (t >= span || page < 0 || page >= v.n_pages) return 0;
+  return t < sinks ? kSink : m != m ? kNan : fkey(m + 0.f);      // (-0 counts as 0)
+}
+
+// The keys and masses of a wave's tokens [first, first + 64 * count): in N registers a
+// lane, or (N = 0) read again each time.
 template <int N>
 struct Keys {
   uint32_t k[N > 0 ? N : 1];
+  float m[N > 0 ? N : 1];
   const PagedView& v;
   const int32_t* table;
   const float* mass;
   int first, count, span, sinks;
 
-  __device__ inline uint32_t read(int j) const {
-    return key_of(v, table, mass, first + 64 * j + (int)(threadIdx.x & 63), span, sinks);
-  }
+  __device__ inline int token(int j) const { return first + 64 * j + (int)(threadIdx.x & 63); }
   __device__ inline void load() {
+    // all loads at once: those behind the last token are of the last
+    int page[N > 0 ? N : 1];
 #pragma unroll
-    for (int j = 0; j < N; ++j) k[j] = j < count ? read(j) : 0;
+    for (int j = 0; j < N; ++j) {
+      const int t = min(token(j), span - 1);
+      m[j] = mass[t];
+      page[j] = table[t >> v.psh];
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) k[j] = j < count ? key_of(v, page[j], m[j], token(j), span, sinks) : 0;
   }
-  // f(key, j) for each of them, in the order of the tokens
+  // f(key, mass, j) for each of them, in the order of the tokens
   template <typename F>
   __device__ inline void each(F f) const {
     if constexpr (N > 0) {
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (j < count) f(k[j], j);
+      for (int j = 0; j < N; ++j) f(k[j], m[j], j);        // (those behind the last are 0)
     } else {
-      for (int j = 0; j < count; ++j) f(read(j), j);
+      for (int j = 0; j < count; ++j) {
+        const int t = min(token(j), span - 1);
+        const float x = mass[t];
+        f(key_of(v, table[t >> v.psh], x, token(j), span, sinks), x, j);
+      }
     }
   }
+  // How many there are of at least `bound`, in all lanes: each lane counts its own
+  // (a ballot and a count of its bits for each 64 keys took three times as long).
   __device__ inline int at_least(uint32_t bound) const {
     int c = 0;
-    each([&](uint32_t x, int) { c += __popcll(__ballot(x >= bound)); });
-    return c;
+    each([&](uint32_t x, float, int) { c += x >= bound; });
+    return wave_sum(c);
   }
 };
 
-// The sum over the block of a count that is the same in all lanes of a wave, and
-// (before) over the waves before this one.
-__device__ inline int block_total(int c, int* sh, int* before = nullptr) {
-  const int w = threadIdx.x >> 6;
-  if ((threadIdx.x & 63) == 0) sh[w] = c;
-  __syncthreads();
-  int all = 0, pre = 0;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    const int x = sh[i];
-    if (i < w) pre += x;
-    all += x;
+// The sums over the block of counts that are the same in all lanes of a wave, each wave's
+// read by a lane of every row; and (before) over the waves before this one.  Calls in
+// a row take the places `sh` by turns.
+using Counts = int2[kWaves];
+struct Totals {
+  int a, b;
+  int2 mine;       // of wave lane % 16
+  __device__ inline int before(int x) const {
+    return __builtin_amdgcn_readfirstlane(row_sum((threadIdx.x & 15) < threadIdx.x >> 6 ? x : 0));
   }
-  if (before) *before = pre;
-  return all;
+};
+static_assert(kWaves == 16, "a lane of a row to each wave");
+__device__ inline Totals block_totals(Counts& sh, int a, int b = 0) {
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = int2{a, b};
+  __syncthreads();
+  const int2 x = sh[threadIdx.x & 15];
+  return Totals{__builtin_amdgcn_readfirstlane(row_sum(x.x)), __builtin_amdgcn_readfirstlane(row_sum(x.y)), x};
 }
+
+// The search for the largest T that K keys reach: the bits above `bit` are settled, met
+// keys are at T or above, over of them behind those that agree with T.
+struct Search {
+  int K;
+  uint32_t T = 0;
+  int met, over = 0, bit = 31;
+  __device__ inline bool done() const { return bit < 0 || met == K; }
+  // The next bit: c keys are at T | 1 << bit or above.
+  __device__ inline uint32_t next() const { return T | 1u << bit; }
+  __device__ inline void settle(int c) {
+    if (c >= K) {
+      T = next();
+      met = c;
+    } else {
+      over = c;
+    }
+    --bit;
+  }
+};
+
+// The most keys of the last rounds, 16 to a lane of one wave.
+constexpr int kCands = 1024;
 
 template <int N>
 __device__ void select(const PagedView& v, const EvictArgs& a, int b, int layer, int n_seqs,
-                       int slot, int n, int (*sh)[kWaves]) {
+                       int slot, int n, Counts* sh, uint32_t* cands) {
   const int want = a.sinks + a.keep, span = n - a.recent;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int per = (span + kThreads - 1) / kThreads;          // groups of 64 tokens of a wave
   const float* mass = mass_row(v, a.mass, layer, slot);
-  Keys<N> keys{{}, v, v.table + (size_t)slot * v.max_pages, mass, w * per * 64, per, span, a.sinks};
+  Keys<N> keys{{}, {}, v, v.table + (size_t)slot * v.max_pages, mass, w * per * 64, per, span, a.sinks};
   keys.load();
-  int turn = 0;                                              // the LDS counts of rounds by turns
-  const int here = block_total(keys.at_least(1), sh[turn++ % 3]);
-  const int sunk = block_total(keys.at_least(kSink), sh[turn++ % 3]);
-  const int K = here - sunk <= a.keep ? here : sunk + a.keep;
-  uint32_t T = 1;
-  if (K < here) {
-    T = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t next = T | 1u << bit;
-      const int c = block_total(keys.at_least(next), sh[turn++ % 3]);
-      if (c >= K) T = next;
-      if (c == K) break;
+  int turn = 0;
+  Totals t = block_totals(sh[turn++ & 1], keys.at_least(1), keys.at_least(kSink));
+  const int here = t.a, K = here - t.b <= a.keep ? here : t.b + a.keep;
+  Search f{K, 0, here};
+  if (K == here) {
+    f.T = 1;
+  } else {
+    while (!f.done() && f.met - f.over > kCands)
+      f.settle(block_totals(sh[turn++ & 1], keys.at_least(f.next())).a);
+    if (!f.done()) {
+      const uint32_t mask = f.bit == 31 ? 0u : ~0u << (f.bit + 1);
+      const auto agrees = [&](uint32_t x) { return x != 0 && (x & mask) == f.T; };
+      int mine = 0;
+      keys.each([&](uint32_t x, float, int) { mine += __popcll(__ballot(agrees(x))); });
+      t = block_totals(sh[turn++ & 1], mine);
+      int at = t.before(t.mine.x);
+      keys.each([&](uint32_t x, float, int) {
+        const uint64_t agree = __ballot(agrees(x));
+        if (agrees(x)) cands[at + __popcll(agree & ((1ull << lane) - 1))] = x;
+        at += __popcll(agree);
+      });
+      __syncthreads();
+      if (w == 0) {
+        uint32_t few[kCands / 64];
+#pragma unroll
+        for (int i = 0; i < kCands / 64; ++i) few[i] = 64 * i + lane < t.a ? cands[64 * i + lane] : 0;
+        const int over = f.over;          // behind all of the few
+        while (!f.done()) {
+          const uint32_t next = f.next();
+          int c = 0;
+#pragma unroll
+          for (int i = 0; i < kCands / 64; ++i) c += few[i] >= next;
+          f.settle(over + wave_sum(c));
+        }
+        if (lane == 0) cands[0] = f.T;
+      }
+      __syncthreads();
+      f.T = cands[0];
     }
   }
+  const uint32_t T = f.T;
   // all above T, and of those at T the first ones
   const int above = T == kSink ? 0 : keys.at_least(T + 1), level = keys.at_least(T) - above;
-  int above_before, level_before;
-  const int most = K - block_total(above, sh[turn++ % 3], &above_before);
-  block_total(level, sh[turn++ % 3], &level_before);
-  int pos = above_before + min(level_before, most), seen = level_before;
+  t = block_totals(sh[turn++ & 1], above, level);
+  const int most = K - t.a;
+  int seen = t.before(t.mine.y), pos = t.before(t.mine.x) + min(seen, most);
   const size_t row = (size_t)layer * n_seqs + b;
   int32_t* idx = a.idx + row * want;
   float* kept = a.kept + row * (want + a.recent);
   if (K > 0)
-    keys.each([&](uint32_t x, int j) {
+    keys.each([&](uint32_t x, float m, int j) {
       const uint64_t below = (1ull << lane) - 1;
       const uint64_t tie = __ballot(x == T);
       const bool take = x > T || (x == T && seen + __popcll(tie & below) < most);
       const uint64_t taken = __ballot(take);
       if (take) {
-        const int t = keys.first + 64 * j + lane, to = pos + __popcll(taken & below);
-        idx[to] = t;
-        kept[to] = mass[t];
+        const int to = pos + __popcll(taken & below);
+        idx[to] = keys.token(j);
+        kept[to] = m;
       }
       pos += __popcll(taken);
       seen += __popcll(tie);
@@ -161,7 +234,8 @@ __device__ void select(const PagedView& v, const EvictArgs& a, int b, int layer,
 }
 
 __global__ __launch_bounds__(kThreads) void evict_select(PagedView v, Slots s, EvictArgs a) {
-  __shared__ int sh[3][kWaves];
+  __shared__ Counts sh[2];
+  __shared__ uint32_t cands[kCands];
   const int b = blockIdx.x % s.n, layer = blockIdx.x / s.n, slot = s.slot[b];
   const int n = seq_len(v, slot);
   const int want = a.sinks + a.keep;
@@ -175,10 +249,10 @@ __global__ __launch_bounds__(kThreads) void evict_select(PagedView v, Slots s, E
     return;
   }
   const int span = n - a.recent;
-  if (span <= 4 * kThreads) select<4>(v, a, b, layer, s.n, slot, n, sh);
-  else if (span <= 16 * kThreads) select<16>(v, a, b, layer, s.n, slot, n, sh);
-  else if (span <= 32 * kThreads) select<32>(v, a, b, layer, s.n, slot, n, sh);
-  else select<0>(v, a, b, layer, s.n, slot, n, sh);
+  if (span <= 4 * kThreads) select<4>(v, a, b, layer, s.n, slot, n, sh, cands);
+  else if (span <= 16 * kThreads) select<16>(v, a, b, layer, s.n, slot, n, sh, cands);
+  else if (span <= 32 * kThreads) select<32>(v, a, b, layer, s.n, slot, n, sh, cands);
+  else select<0>(v, a, b, layer, s.n, slot, n, sh, cands);
 }
 
 // The masses that stay, where the rows were compacted; one (layer, sequence) to
