@@ -111,9 +111,12 @@ __device__ inline uint32_t from_fp4(uint32_t w, float scale) {
 
 __device__ inline float max4(f32x4 v) { return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])); }
 
-__device__ inline uint32_t bf16_pair(float lo, float hi) {
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)lo, (__bf16)hi});
+// The largest over the four lanes of the same l16, in all of them.
+__device__ inline float quads_max(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 // Any of the lane's V elements an infinity or NaN.
@@ -152,8 +155,8 @@ __device__ inline void zero_not_finite(R& r) {
 // conversion, two at a time, as the fragments are made, and all else is the
 // same.  K's products may take the elements of a row in any order that Q's take
 // too: lane quad holds the D/4 neighbouring ones that it reads at once, which are
-// of one scale.
-template <typename T, int D, int NB, bool F4 = false>
+// of one scale.  kOnePage: pages of 32 tokens or more, so that a step lies in one.
+template <typename T, int D, int NB, bool F4 = false, bool kOnePage = false>
 __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArgs a, AttendLists s,
                                                        unsigned run) {
   using F = Frag<T>;
@@ -233,23 +236,32 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
   }
   // 4 bits: a step's rows are read while the step before is worked on
   [[maybe_unused]] Fp4Step<D> ahead;
+  // the lane's bytes behind those of a half's first row
+  [[maybe_unused]] const uint32_t k_at = l16 * (D / 2) + quad * (D / 8);
+  [[maybe_unused]] const uint32_t ks_at = l16 * (D / 32) + quad * (D / 4) / 32;
+  [[maybe_unused]] const uint32_t v_at = 4 * quad * (D / 2) + l16 * (D / 32), vs_at = 4 * quad * (D / 32);
   [[maybe_unused]] const auto fetch = [&](int w, int p0, int p1) {
+    using S = Fp4Step<D>;
     const int at0 = step_token<kStep>(ts, min(w, ts.nt - 1));
+    const char *kr, *vr, *ksr, *vsr;       // a half's first rows and their scales
+    const auto rows_at = [&](int page, int in_page) {
+      const int64_t at = base + (int64_t)(page >= 0 && page < v.n_pages ? page : 0) * v.ps;
+      kr = v.k + at + in_page * (D / 2);
+      vr = v.v + at + in_page * (D / 2);
+      ksr = v.k + at + v.P * (D / 2) + in_page * (D / 32);
+      vsr = v.v + at + v.P * (D / 2) + in_page * (D / 32);
+    };
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      using S = Fp4Step<D>;
-      const int page = h ? p1 : p0, in_page = (at0 + 16 * h) & (v.P - 1);
-      const int64_t at = base + (int64_t)(page >= 0 && page < v.n_pages ? page : 0) * v.ps;
-      const char* kr = v.k + at + in_page * (D / 2);
-      const char* vr = v.v + at + in_page * (D / 2);
-      const int scales = v.P * (D / 2) - in_page * (D / 2 - D / 32);   // from kr and vr on
-      ahead.k[h] = *reinterpret_cast<const typename S::KRow*>(kr + l16 * (D / 2) + quad * (D / 8));
-      ahead.ks[h] = *reinterpret_cast<const uint8_t*>(kr + scales + l16 * (D / 32) + quad * (D / 4) / 32);
+      if (h == 0 || !kOnePage) rows_at(h ? p1 : p0, (at0 + 16 * h) & (v.P - 1));
+      const uint32_t more = kOnePage ? h : 0;      // 16 rows behind kr and vr
+      ahead.k[h] = *reinterpret_cast<const typename S::KRow*>(kr + (k_at + more * 8 * D));
+      ahead.ks[h] = *reinterpret_cast<const uint8_t*>(ksr + (ks_at + more * (D / 2)));
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        ahead.v[4 * h + j] = *reinterpret_cast<const typename S::VRow*>(
-            vr + (4 * quad + j) * (D / 2) + l16 * (D / 32));
-      ahead.vs[h] = *reinterpret_cast<const typename S::Scales*>(vr + scales + 4 * quad * (D / 32));
+        ahead.v[4 * h + j] =
+            *reinterpret_cast<const typename S::VRow*>(vr + (v_at + more * 8 * D + j * (D / 2)));
+      ahead.vs[h] = *reinterpret_cast<const typename S::Scales*>(vsr + (vs_at + more * (D / 2)));
     }
   };
   int page0 = next0, page1 = next1;     // 4 bits: this step's pages
@@ -257,7 +269,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
     if (u < u1) {
       fetch(u, next0, next1);
       next0 = page_of(u + kWaves, 0);
-      next1 = page_of(u + kWaves, 1);
+      next1 = kOnePage ? next0 : page_of(u + kWaves, 1);
     }
   }
   for (; u < u1; u += kWaves) {
@@ -284,13 +296,14 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
           kf[h][f] = __builtin_bit_cast(frag, u32x4{from_fp4<0>(w, ks), from_fp4<1>(w, ks),
                                                     from_fp4<2>(w, ks), from_fp4<3>(w, ks)});
         }
-        // the byte of the lane's columns among each row's scales
+        // the byte of the lane's columns among each row's scales, turned to where a
+        // float's exponent lies; the conversion looks at nothing else of it
         constexpr int kPer = D / 32;
         const int byte = l16 * kPer / 16;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint32_t sw = reinterpret_cast<const uint32_t(&)[kPer]>(ahead.vs[h])[j * kPer / 4];
-          const float vs = __uint_as_float((sw >> (8 * byte + j * kPer % 4 * 8) & 0xFFu) << 23);
+          const float vs = __uint_as_float(__builtin_amdgcn_alignbit(sw, sw, 8 * byte + j * kPer % 4 * 8 + 9));
           const uint32_t w = ahead.v[4 * h + j];
           vv[4 * h + j][0][0] = from_fp4<0>(w, vs);
           vv[4 * h + j][0][1] = from_fp4<1>(w, vs);
@@ -304,7 +317,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
       page1 = next1;
       if (u + kWaves < u1) fetch(u + kWaves, page0, page1);
       next0 = page_of(u + 2 * kWaves, 0);
-      next1 = page_of(u + 2 * kWaves, 1);
+      next1 = kOnePage ? next0 : page_of(u + 2 * kWaves, 1);
     } else {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -362,8 +375,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       float mt = fmaxf(max4(x[nb][0]), max4(x[nb][1]));
-      mt = fmaxf(mt, __shfl_xor(mt, 16));
-      mt = fmaxf(mt, __shfl_xor(mt, 32));
+      mt = quads_max(mt);
       const float mn = fmaxf(m[nb], mt);
       const float ms = mn == -INFINITY ? 0.f : mn;     // a row that saw nothing yet
       const float alpha = __builtin_amdgcn_exp2f((m[nb] - ms) * a.scale);
@@ -584,10 +596,19 @@ int launch(const PagedView& v, const AttendArgs& a, const AttendLists& l, const 
   if (s.many) {
     const int err = launch_attend_many(v, a, l, s, st);
     if (err) return err;
-  } else if (s.row_tile == 16) {
-    attend_few<T, D, 1, F4><<<blocks, kThreads, 0, st>>>(v, a, l, run);
-  } else if constexpr (sizeof(T) == 2) {
-    attend_few<T, D, 2, F4><<<blocks, kThreads, 0, st>>>(v, a, l, run);
+  } else {
+    const auto go = [&](auto kernel) { kernel<<<blocks, kThreads, 0, st>>>(v, a, l, run); };
+    const auto by_rows = [&](auto one_page) {
+      constexpr bool kOnePage = decltype(one_page)::value;
+      if (s.row_tile == 16) go(attend_few<T, D, 1, F4, kOnePage>);
+      else if constexpr (sizeof(T) == 2) go(attend_few<T, D, 2, F4, kOnePage>);
+    };
+    if constexpr (F4) {
+      if (v.P >= kStep) by_rows(std::true_type{});
+      else by_rows(std::false_type{});
+    } else {
+      by_rows(std::false_type{});
+    }
   }
   if (s.n_split > 1) {
     // up to four splits for each thread
