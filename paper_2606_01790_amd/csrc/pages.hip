@@ -314,21 +314,25 @@ __global__ __launch_bounds__(256) void write_fp4(PagedView v, Rows<N> r, WriteAr
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     const int part = (int)(i % VPR);
     const int64_t rg = i / VPR;
-    const int g = (int)(rg % v.G), row = (int)(rg / v.G);
+    const int g = (int)((uint32_t)rg % (uint32_t)v.G), row = (int)((uint32_t)rg / (uint32_t)v.G);
+    // the rows first, whether they are to be written or not: their way overlaps that of
+    // the page
+    const int64_t from = (int64_t)layer * a.ls + (int64_t)g * a.gs + (int64_t)row * a.ts + part * 16;
+    const i32x4 kk = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(a.k + from));
+    const i32x4 vv = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(a.v + from));
     const int b = owner_of(r.row0, r.n, row);
     if (a.grown && a.grown[b] != STARKV_SEQ_OK) continue;
     const int t = seq_len(v, r.slot[b]) - r.row0[b + 1] + row;
     if (t < 0) continue;
     const int page = table_row(v, r.slot[b])[t >> v.psh];
     if (!is_page(v, page) || v.refs[page] > 1) continue;
-    const int64_t from = (int64_t)layer * a.ls + (int64_t)g * a.gs + (int64_t)row * a.ts + part * 16;
     const int64_t block = (int64_t)layer * v.ls + (int64_t)page * v.ps + (int64_t)g * v.gs;
     const int in_page = t & (v.P - 1);
     const int64_t to = block + (int64_t)in_page * (D / 2) + part * 4;
     const int64_t sto = block + (int64_t)v.P * (D / 2) + in_page * (D / 32) + part / 4;
     uint32_t ks, vs;
-    const uint32_t kc = quantise(*reinterpret_cast<const i32x4*>(a.k + from), &ks);
-    const uint32_t vc = quantise(*reinterpret_cast<const i32x4*>(a.v + from), &vs);
+    const uint32_t kc = quantise(kk, &ks);
+    const uint32_t vc = quantise(vv, &vs);
     *reinterpret_cast<uint32_t*>(v.k + to) = kc;
     *reinterpret_cast<uint32_t*>(v.v + to) = vc;
     if (part % 4 == 0) {
@@ -363,7 +367,7 @@ __global__ __launch_bounds__(256) void read_kernel(PagedView v, Rows<N> r, ReadA
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     const int part = (int)(i % kOut);
     const int64_t rg = i / kOut;
-    const int g = (int)(rg % v.G), row = (int)(rg / v.G);
+    const int g = (int)((uint32_t)rg % (uint32_t)v.G), row = (int)((uint32_t)rg / (uint32_t)v.G);
     const int b = owner_of(r.row0, r.n, row);
     const int t = seq_len(v, r.slot[b]) - r.row0[b + 1] + row;
     const int page = t < 0 ? -1 : table_row(v, r.slot[b])[t >> v.psh];
@@ -383,8 +387,8 @@ __global__ __launch_bounds__(256) void read_kernel(PagedView v, Rows<N> r, ReadA
       }
     }
     const int64_t to = (int64_t)layer * a.ls + (int64_t)g * a.gs + (int64_t)row * a.ts + part * 16;
-    *reinterpret_cast<i32x4*>(a.k + to) = kk;
-    *reinterpret_cast<i32x4*>(a.v + to) = vv;
+    __builtin_nontemporal_store(kk, reinterpret_cast<i32x4*>(a.k + to));
+    __builtin_nontemporal_store(vv, reinterpret_cast<i32x4*>(a.v + to));
   }
 }
 
