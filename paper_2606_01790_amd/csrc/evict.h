@@ -56,7 +56,5 @@ struct EvictCall {
   float* kept;
 };
 int launch_evict_select(const PagedView& v, const EvictCall& c, void* stream);
-int launch_evict_masses(const PagedView& v, const EvictCall& c, const int32_t* status,
-                        void* stream);
 
 }  // namespace starkv

@@ -1,6 +1,6 @@
 // Eviction by accumulated attention weight: of a sequence's masses the largest,
-// in the order of their tokens, and the masses moved to where the compaction
-// moved their rows.
+// in the order of their tokens.  The compaction moves their rows, and their masses
+// from where they are put aside here.
 //
 // One block of 16 waves works on a (layer, sequence).  The masses become 32-bit
 // keys in the order of the numbers, a wave keeps a range of tokens' keys in its
@@ -255,18 +255,7 @@ __global__ __launch_bounds__(kThreads) void evict_select(PagedView v, Slots s, E
   else select<0>(v, a, b, layer, s.n, slot, n, sh, cands);
 }
 
-// The masses that stay, where the rows were compacted; one (layer, sequence) to
-// a row of blocks.
-__global__ __launch_bounds__(256) void evict_masses(PagedView v, Slots s, EvictArgs a,
-                                                    const int32_t* status) {
-  const int b = blockIdx.x % s.n, layer = blockIdx.x / s.n;
-  if (status[b] != STARKV_SEQ_OK) return;
-  const int n = a.counts[b] + a.recent;
-  const float* kept = a.kept + ((size_t)layer * s.n + b) * (a.sinks + a.keep + a.recent);
-  float* mass = mass_row(v, a.mass, layer, s.slot[b]);
-  for (int i = blockIdx.y * 256 + threadIdx.x; i < n; i += gridDim.y * 256) mass[i] = kept[i];
-}
-
+// Masses of a forked sequence, a row of blocks to a (layer, sequence).
 __global__ __launch_bounds__(256) void mass_fork(PagedView v, Slots s, float* mass) {
   const int b = blockIdx.x % s.n, layer = blockIdx.x / s.n;
   const int n = seq_len(v, s.from[b]);
@@ -298,15 +287,6 @@ unsigned row_blocks(int64_t pairs, int64_t n) {
 int launch_evict_select(const PagedView& v, const EvictCall& c, void* stream) {
   evict_select<<<(unsigned)(v.n_layers * c.s.n), kThreads, 0, reinterpret_cast<hipStream_t>(stream)>>>(
       v, slots_of(c.s), args_of(c));
-  return (int)hipGetLastError();
-}
-
-int launch_evict_masses(const PagedView& v, const EvictCall& c, const int32_t* status,
-                        void* stream) {
-  const int64_t pairs = (int64_t)v.n_layers * c.s.n;
-  const dim3 grid((unsigned)pairs, row_blocks(pairs, (int64_t)c.keep + c.sinks + c.recent));
-  evict_masses<<<grid, 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(v, slots_of(c.s), args_of(c),
-                                                                        status);
   return (int)hipGetLastError();
 }
 

@@ -196,11 +196,11 @@ starkv_status starkv_pages_evict(const starkv_paged* cache, const int32_t* slots
   c.stay = reinterpret_cast<int32_t*>(p + w.stay);
   c.kept = reinterpret_cast<float*>(p + w.kept);
   c.s.grown = c.stay;
+  c.s.kept = KeptMasses{c.kept, mass};
   int err = launch_evict_select(v, c, stream);
   if (!err)
     err = launch_pages_compact(v, c.s, true, idx, (int64_t)n * want, want, c.counts, recent,
                                w.pages, status, ws, stream);
-  if (!err) err = launch_evict_masses(v, c, status, stream);
   return hip_status(err);
 }
 

@@ -31,12 +31,19 @@ struct PagedView {
   bool fp4 = false;
 };
 
+// The masses that stay in an eviction, [n_layers][n][B + tail], and the cache's.
+struct KeptMasses {
+  const float* from = nullptr;
+  float* to = nullptr;
+};
+
 // The sequences of a call, passed to the kernels by value.
 struct SeqList {
   int32_t n;
   int32_t slot[kMaxSeqs];
   int32_t num[kMaxSeqs];    // per sequence: tokens added, a span, or the slot forked from
   const int32_t* grown = nullptr;   // compact, device: the status of the grow before it, if any
+  KeptMasses kept;                  // compact: that move too, if any
 };
 
 // Rows of the sequences of a call: sequence b has rows [row0[b], row0[b+1]).

@@ -533,6 +533,7 @@ struct MoveArgs {
   const int32_t* idx;
   int64_t idx_ls;
   int B, tail, chunks;
+  KeptMasses kept;
 };
 
 // The kept rows into the fresh pages, one vector of K and of V per thread
@@ -547,6 +548,11 @@ __global__ __launch_bounds__(256) void compact_move(PagedView v, Seqs<N> s, Move
   const i32x4 info = m.info[b];
   const int len0 = info[0], a = info[1], cnt = info[2];
   if (cnt < 0) return;
+  if (m.kept.from && chunk == 0 && g == 0) {      // (an eviction's masses move with the rows)
+    const float* from = m.kept.from + ((size_t)layer * s.n + b) * (m.B + m.tail);
+    float* to = m.kept.to + ((size_t)layer * v.n_slots + s.slot[b]) * v.cap;
+    for (int i = threadIdx.x; i < cnt + m.tail; i += 256) to[i] = from[i];
+  }
   const int r0 = info[3] << v.psh;                 // the first fresh page's first token
   const int64_t nvec = ((int64_t)a + cnt + m.tail - r0) * VPR;
   const int32_t* idx = m.idx + (int64_t)layer * m.idx_ls + (int64_t)b * m.B;
@@ -704,6 +710,7 @@ int launch_pages_compact(const PagedView& v, const SeqList& s, bool whole, const
   m.idx_ls = idx_ls;
   m.B = B;
   m.tail = tail;
+  m.kept = s.kept;
   with_list(s, [&](const auto& l) {
     compact_plan<<<1, kPlanThreads, 0, st>>>(v, l, whole, B, counts, tail, s.grown,
                                              reinterpret_cast<int32_t*>(p + w.fresh),

@@ -41,3 +41,20 @@ def cache_of(m, H, d, order="plain"):
 def empty_model(nl, n_pages, G, P, d, n_slots, max_pages, fill=255):
     pool = np.full((nl, n_pages, G, P, EO.fp4_row_bytes(d)), fill, dtype=np.uint8)
     return PO.PagedModel(pool, pool.copy(), n_slots, max_pages)
+
+
+def model_of(c):
+    """The host model with what a cache holds now (rows of a plain one in fp64), and what
+    makes its rows numbers."""
+    if c.fp4:
+        n, out = c.page_tokens * c.d // 2, []
+        for t in (c.k, c.v):
+            x = t.cpu().numpy()
+            lead = x.shape[:3]
+            out.append(np.concatenate([x[..., :n].reshape(*lead, -1, c.d // 2),
+                                       x[..., n:].reshape(*lead, -1, c.d // 32)], -1))
+    else:
+        out = [t.double().cpu().numpy() for t in (c.k, c.v)]
+    m = PO.PagedModel(*out, *c.table.shape)
+    m.table, m.len, m.refs = c.table.cpu().numpy(), c.length.cpu().numpy(), c.refs.cpu().numpy()
+    return m, EO.fp4_numbers if c.fp4 else lambda x: x

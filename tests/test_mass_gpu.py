@@ -281,6 +281,14 @@ def test_heads_of_a_group():
         run(f"H {H} G {G}", Case(31 + H, [70, 5], [T, 1], H, G, 64, 16, dtype))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32", "fp4"])
+def test_many_groups_and_large_tiles(dtype):
+    """64 groups, and by the bound so many tokens that tiles have four parts: the most
+    LDS."""
+    lens, rows = [20 + i % 25 for i in range(118)] + [150, 1700], [1] * 119 + [0]
+    run("64 groups", Case(3, lens, rows, 64, 64, 64, 16, dtype))
+
+
 def test_layer_by_layer_and_streams():
     c = Case(16, [300, 77], [3, 3], 8, 2, 64, 16, nl=3)
     c.upload()
