@@ -31,16 +31,18 @@ starkv_status mass_shape(const PagedView& v, const int32_t* rows, int n, int32_t
   if (tot > kMaxTokens) return STARKV_E_PARAM;
   s->n_rows = (int)tot;
   const int64_t R = most * hpg;
-  s->many = v.esz == 2 && R > 32;
+  s->many = R > 32;
   s->row_blocks = (int)std::max<int64_t>(1, (R + 15) / 16);
   const int64_t len = std::min<int64_t>(max_len, v.cap);
   const int64_t pairs = std::max<int64_t>(1, (int64_t)v.n_layers * n);
   s->n_split = 1;
   s->ws_bytes = 0;
   if (!s->many) {
-    // tiles of four parts, or of one where those are too few for the card
-    const int part = v.fp4 ? 32 : 16;
-    s->tile = pairs * ((len + 4 * part - 1) / (4 * part)) >= 512 ? 4 * part : part;
+    // tiles of four parts of every group (of 256 tokens where there are fewer than four
+    // groups, so that a wave has more than one), or of one where those are too few for
+    // the card
+    const int part = v.fp4 ? 32 : 16, most = v.G < 4 ? 256 : 4 * part;
+    s->tile = pairs * ((len + most - 1) / most) >= 512 ? most : part;
     s->tiles = (int)((len + s->tile - 1) / s->tile);
     s->blocks = (int)std::min<int64_t>(pairs * s->tiles, 1 << 20);   // (the launch takes what the card holds)
     return STARKV_OK;
@@ -49,12 +51,12 @@ starkv_status mass_shape(const PagedView& v, const int32_t* rows, int n, int32_t
   s->tiles = (int)((len + s->tile - 1) / s->tile);
   s->blocks = (int)std::max<int64_t>(1, std::min<int64_t>(s->tiles, (1 << 22) / pairs));
   // splits of a tile's (group, 32 rows) products until there are 2,048 blocks, of
-  // at least 16 products; a multiple of the 8 XCDs, each of which then reads the
+  // at least four products; a multiple of the 8 XCDs, each of which then reads the
   // same eighth of Q for every tile (2,755 rows over 13,711 tokens: 32, 40 or 48
   // splits 287 us, 37 298, 16 290, 9 310)
   const int64_t products = v.G * ((R + 31) / 32);
   s->n_split = (int)std::max<int64_t>(
-      1, std::min({2048 / (pairs * s->tiles), products / 16, (int64_t)64}));
+      1, std::min({2048 / (pairs * s->tiles), products / 4, (int64_t)64}));
   if (s->n_split > 8) s->n_split &= ~7;
   if (s->n_split > 1)
     s->ws_bytes = (size_t)pairs * s->n_split * s->tiles * s->tile * sizeof(float);

@@ -9,9 +9,8 @@
 // end, and what lies in a token's place that nobody should see (no page, behind
 // the last) spoils no other token.
 //
-// Few rows (a decoded token, a few drafted ones; float32 of any number) are bound
-// by HBM: mass_few takes tiles of 64 tokens, K straight to registers, and adds up the
-// groups through LDS.
+// Few rows (a decoded token, a few drafted ones) are bound by HBM: mass_few takes
+// tiles of tokens, K straight to registers, and adds up the groups through LDS.
 // Many rows are bound by the matrix units and the exponentials: mass_many keeps 64
 // tokens' K in a wave's registers and walks the rows, which all waves read from
 // LDS, groups one after the other into the same sums.
@@ -256,13 +255,12 @@ struct Tiles {
   }
 };
 
-// A block takes tiles of S parts of a group (four, or one where those tiles are too few;
-// a part is 16 tokens, 32 in 4 bits, whose rows are shorter), and of all groups' parts
-// each wave a quarter, whole groups first.  The next part's K is on its way while one is worked
+// A block takes tiles of S parts of a group (a part is 16 tokens, 32 in 4 bits, whose rows
+// are shorter), and of all groups' parts each wave a quarter, whole groups first.  The next part's K is on its way while one is worked
 // on, across tiles.  NB: the 16-row blocks of every sequence, which stay in registers
-// while the group does; 0: any number, read for each part.
-template <typename T, int D, int NB>
-constexpr int kResident = sizeof(T) == 4 && D == 128 ? (NB == 2 ? 2 : 3) : NB == 1 ? 5 : 4;   // blocks of a CU
+// while the group does.
+template <typename T, int D, int NB>      // blocks of a CU
+constexpr int kResident = sizeof(T) == 4 && D == 128 ? (NB == 2 ? 2 : 3) : NB == 1 ? 5 : 4;
 template <bool F4>
 constexpr int kPart = F4 ? 32 : 16;
 template <typename T, int D, bool F4, int NB, int S>
@@ -297,14 +295,14 @@ __global__ __launch_bounds__(kThreads, (kResident<T, D, NB>)) void mass_few(Page
     const int te = min(t0 + kTokens, s.n);
     whole = te - 1 <= s.first && (t0 > s.n - 1 - a.window || te <= a.sinks);
   };
-  Rows16<T, D, F4> rows[NB > 0 ? NB : 1];
+  Rows16<T, D, F4> rows[NB];
   int row_layer = -1, row_slot = -1, row_g = -1;
   // the wave's next part, K of which is in `k`; K of the one behind it comes into
   // `ahead`.  False behind the last
   const auto step = [&](K& k, K& ahead) {
     const int g = part / S;
     const bool last = part + 1 >= p1;
-    if (NB > 0 && part < p1 && (g != row_g || s.slot != row_slot || s.layer != row_layer)) {
+    if (part < p1 && (g != row_g || s.slot != row_slot || s.layer != row_layer)) {
 #pragma unroll
       for (int i = 0; i < NB; ++i) rows[i].load(v, a, s, g, 16 * i);
       __builtin_amdgcn_s_waitcnt(0x0F70);   // here, and not behind the next K below
@@ -321,16 +319,8 @@ __global__ __launch_bounds__(kThreads, (kResident<T, D, NB>)) void mass_few(Page
       for (int h = 0; h < kHalves; ++h) {
         const int in_tile = kPart<F4> * (part % S) + 16 * h + l16, t = t0 + in_tile;
         float sum = 0.f;
-        if constexpr (NB > 0) {
 #pragma unroll
-          for (int i = 0; i < NB; ++i) sum += rows[i].weigh(a, k.half[h], t, whole);
-        } else {
-          // (the rows that lie before the tile do not see it)
-          for (int r0 = max(t0 - s.first, 0) * s.hpg & ~15; r0 < s.R; r0 += 16) {
-            rows[0].load(v, a, s, g, r0);
-            sum += rows[0].weigh(a, k.half[h], t, whole);
-          }
-        }
+        for (int i = 0; i < NB; ++i) sum += rows[i].weigh(a, k.half[h], t, whole);
         sum = quads_sum(sum);
         if (quad == 0) mine[g * kTokens + in_tile] = sum;
       }
@@ -372,6 +362,49 @@ __device__ constexpr int q_swizzle(int row) {
   return D == 128 ? row & 15 : (row >> 1) & 7;
 }
 
+// What a block does of a tile: `w0` to `w1` of the products of 32 rows of a group that
+// see some of it, group after group.
+struct Share {
+  int t0;            // the tile's first token
+  int p0, p1;        // products of a group
+  int64_t w0, w1;
+  bool joined;       // its sums are added to other blocks' afterwards
+
+  // False: nothing, others do it.
+  __device__ inline bool take(const PagedView& v, const MassArgs& a, const Seq& s, int tile, int split) {
+    // tiles behind the bound that the splits' sums were sized by are not split
+    joined = a.n_split > 1 && tile < a.tiles;
+    if (!joined && split) return false;
+    t0 = tile * kTile;
+    // from the row at t0 to the last one whose window reaches back to the tile's end
+    const int t1 = min(t0 + kTile, s.n), i0 = max(t0 - s.first, 0);
+    const int64_t reach = t0 < a.sinks ? s.T - 1 : (int64_t)t1 - 1 + a.window - 1 - s.first;
+    const int i1 = (int)min(reach, (int64_t)s.T - 1);
+    p0 = i0 * s.hpg / 32;
+    p1 = i1 < i0 ? p0 : ((i1 + 1) * s.hpg + 31) / 32;
+    const int64_t all = (int64_t)v.G * (p1 - p0);
+    w0 = joined ? all * split / a.n_split : 0;
+    w1 = joined ? all * (split + 1) / a.n_split : all;
+    return true;
+  }
+  // The products [from, to) of the next group.
+  __device__ inline bool next(int* g, int* from, int* to) {
+    if (w0 >= w1) return false;
+    *g = (int)(w0 / (p1 - p0));
+    *from = p0 + (int)(w0 - (int64_t)*g * (p1 - p0));
+    *to = (int)min((int64_t)p1, *from + w1 - w0);
+    w0 += *to - *from;
+    return true;
+  }
+  __device__ inline void store(const PagedView& v, const MassArgs& a, const Seq& s, int pair, int split,
+                               int t, float add) const {
+    if (joined)
+      a.part[((size_t)pair * a.n_split + split) * a.tiles * kTile + t] = add;
+    else if (t < s.n)
+      store_mass(v, a, s, t, add);
+  }
+};
+
 template <int D, bool F4>
 __global__ __launch_bounds__(kThreads, 2) void mass_many(PagedView v, MassArgs a, RowList r) {
   constexpr int NF = D / 16, NP = D / 8, kRow = D * 2;
@@ -394,26 +427,12 @@ __global__ __launch_bounds__(kThreads, 2) void mass_many(PagedView v, MassArgs a
   const uint32_t per_head = (uint32_t)(((1ull << 32) + s.hpg - 1) / s.hpg);
 
   for (int tile = at % a.blocks; (int64_t)tile * kTile < s.n; tile += a.blocks) {
-    // tiles behind the bound that the splits' sums were sized by are not split
-    const bool shared_tile = a.n_split > 1 && tile < a.tiles;
-    if (!shared_tile && split) continue;
-    const int t0 = tile * kTile, t1 = min(t0 + kTile, s.n);
-    // the 32-row products of each group that see some of the tile: from the row
-    // at t0 to the last one whose window reaches back to t1 - 1
-    const int i0 = max(t0 - s.first, 0);
-    const int64_t reach = t0 < a.sinks ? s.T - 1 : (int64_t)t1 - 1 + a.window - 1 - s.first;
-    const int i1 = (int)min(reach, (int64_t)s.T - 1);
-    const int p0 = i0 * s.hpg / 32, p1 = i1 < i0 ? p0 : ((i1 + 1) * s.hpg + 31) / 32;
-    const int64_t all = (int64_t)v.G * (p1 - p0);
-    int64_t w0 = shared_tile ? all * split / a.n_split : 0;
-    const int64_t w1 = shared_tile ? all * (split + 1) / a.n_split : all;
-
+    Share share;
+    if (!share.take(v, a, s, tile, split)) continue;
+    const int t0 = share.t0;
     float sum[2][2] = {};
-    while (w0 < w1) {
-      const int g = (int)(w0 / (p1 - p0));
-      const int from = p0 + (int)(w0 - (int64_t)g * (p1 - p0));
-      const int to = (int)min((int64_t)p1, from + w1 - w0);
-      w0 += to - from;
+    int g, from, to;
+    while (share.next(&g, &from, &to)) {
       // K of the wave's tokens: a lane holds half a row of tokens l32 and 32 + l32
       bf16x8 kf[2][NF];
 #pragma unroll
@@ -575,11 +594,51 @@ __global__ __launch_bounds__(kThreads, 2) void mass_many(PagedView v, MassArgs a
       sum[h][0] += __shfl_xor(sum[h][0], 32);
     }
     const int t = t0 + 64 * wave + lane;
-    const float add = half ? sum[1][0] : sum[0][0];
-    if (shared_tile)
-      a.part[((size_t)pair * a.n_split + split) * a.tiles * kTile + t] = add;
-    else if (t < s.n)
-      store_mass(v, a, s, t, add);
+    share.store(v, a, s, pair, split, t, half ? sum[1][0] : sum[0][0]);
+  }
+}
+
+// float32: as above, with a wave's 64 tokens as four times 16 and the rows straight to
+// registers, 16 at a time: the matrix units take 16 times as long for a row as in bf16,
+// and a CU's other waves have them while one waits.
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void mass_many_f32(PagedView v, MassArgs a, RowList r) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int split = blockIdx.x % a.n_split, at = blockIdx.x / a.n_split;
+  const int pair = at / a.blocks, b = pair % r.n, layer = pair / r.n;
+  const Seq s = seq_of(v, r, layer, b);
+  if (s.T == 0) return;
+  for (int tile = at % a.blocks; (int64_t)tile * kTile < s.n; tile += a.blocks) {
+    Share share;
+    if (!share.take(v, a, s, tile, split)) continue;
+    const int tw = share.t0 + 64 * wave, te = min(tw + 64, s.n);      // the wave's tokens
+    float sum[4] = {};
+    int g, from, to;
+    while (share.next(&g, &from, &to)) {
+      KRow<float, D, false> k[4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const int t = min(tw + 16 * h + l16, s.n - 1), page = table_of(v, s)[t >> v.psh];
+        k[h].load(v, v.k + (int64_t)layer * v.ls + (int64_t)(is_page(v, page) ? page : 0) * v.ps +
+                         (int64_t)g * v.gs,
+                  t & (v.P - 1), quad, v.ts);
+      }
+      const int end = min(32 * to, s.R);
+      for (int r0 = 32 * from; r0 < end; r0 += 16) {
+        Rows16<float, D, false> rows;
+        rows.load(v, a, s, g, r0);
+        const int p_first = s.first + r0 / s.hpg, p_last = s.first + min(r0 + 15, s.R - 1) / s.hpg;
+        const bool whole = te - 1 <= p_first && (tw > p_last - a.window || te <= a.sinks);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) sum[h] += rows.weigh(a, k[h], tw + 16 * h + l16, whole);
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 4; ++h) sum[h] = quads_sum(sum[h]);
+    // lane l16 of quad h writes token 16 h + l16
+    const float lo = quad & 1 ? sum[1] : sum[0], hi = quad & 1 ? sum[3] : sum[2];
+    share.store(v, a, s, pair, split, tw + lane, quad & 2 ? hi : lo);
   }
 }
 
@@ -629,7 +688,8 @@ int launch_mass_add(const PagedView& v, const MassCall& c, void* stream) {
     const unsigned pairs = (unsigned)(v.n_layers * c.r.n);
     const unsigned blocks = pairs * c.s.blocks * c.s.n_split;
     const auto go = [&](auto kernel) { kernel<<<blocks, kThreads, 0, st>>>(v, a, c.r); };
-    if (v.d == 128) v.fp4 ? go(mass_many<128, true>) : go(mass_many<128, false>);
+    if (v.esz == 4) v.d == 128 ? go(mass_many_f32<128>) : go(mass_many_f32<64>);
+    else if (v.d == 128) v.fp4 ? go(mass_many<128, true>) : go(mass_many<128, false>);
     else v.fp4 ? go(mass_many<64, true>) : go(mass_many<64, false>);
     if (c.s.n_split > 1) {
       const unsigned parts = (unsigned)std::min(c.s.tiles, std::max(1, (int)(2048 / pairs)));
@@ -644,13 +704,14 @@ int launch_mass_add(const PagedView& v, const MassCall& c, void* stream) {
     constexpr bool F4 = decltype(f4)::value;
     const unsigned blocks = (unsigned)std::min<int64_t>(c.s.blocks, 256 * kResident<T, D, NB>);
     const auto go = [&](auto kernel) { kernel<<<blocks, kThreads, lds, st>>>(v, a, c.r); };
-    c.s.tile == kPart<F4> ? go(mass_few<T, D, F4, NB, 1>) : go(mass_few<T, D, F4, NB, 4>);
+    if (c.s.tile == kPart<F4>) go(mass_few<T, D, F4, NB, 1>);
+    else if (c.s.tile == 4 * kPart<F4>) go(mass_few<T, D, F4, NB, 4>);
+    else go(mass_few<T, D, F4, NB, kThreads / kPart<F4>>);
   };
   const auto by_rows = [&](auto t, auto d, auto f4) {
     using T = typename decltype(t)::type;
     if (c.s.row_blocks == 1) by_tile(t, d, f4, Int<1>{});
-    else if (sizeof(T) == 2 || c.s.row_blocks == 2) by_tile(t, d, f4, Int<2>{});
-    else if constexpr (sizeof(T) == 4) by_tile(t, d, f4, Int<0>{});
+    else by_tile(t, d, f4, Int<2>{});
   };
   const auto by_type = [&](auto d) {
     if (v.fp4) by_rows(Type<__bf16>{}, d, std::true_type{});

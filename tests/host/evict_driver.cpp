@@ -126,7 +126,7 @@ int main() {
       }
       CHECK(mass.r.n == n && mass.r.row0[n] == tot && s.n_rows == tot);
       const int64_t pairs = (int64_t)c.n_layers * n, len = std::min(max_len, cap);
-      CHECK(s.many == (c.dtype != STARKV_F32 && R > 32));
+      CHECK(s.many == (R > 32));
       CHECK((int64_t)s.tiles * s.tile >= len && (int64_t)(s.tiles - 1) * s.tile < len);
       CHECK(s.blocks >= 1 && s.n_split >= 1);
       if (s.many) {
@@ -137,8 +137,8 @@ int main() {
         split += s.n_split > 1;
       } else {
         const int part = v.fp4 ? 32 : 16;
-        CHECK((s.tile == part || s.tile == 4 * part) && s.n_split == 1 && s.ws_bytes == 0);
-        CHECK((int64_t)s.row_blocks * 16 >= R && (v.esz == 4 || s.row_blocks <= 2));
+        CHECK((s.tile == part || s.tile == (c.G < 4 ? 256 : 4 * part)) && s.n_split == 1 && s.ws_bytes == 0);
+        CHECK((int64_t)s.row_blocks * 16 >= R && s.row_blocks <= 2);
         CHECK(2 * c.G * s.tile * 4 <= 64 * 1024);       // LDS
       }
       CHECK(s.ws_bytes == ws && (!ws || mass.part == f32));

@@ -183,7 +183,17 @@ def test_short_and_long_bounds(dtype, T):
         assert torch.equal(a, c.out)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "fp4"])
+@pytest.mark.parametrize("G", [1, 2, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "fp4", "f32"])
+def test_whole_tiles_of_few_groups(dtype, G):
+    """Enough tiles for the card: of 256 tokens below four groups, of four parts from
+    there on."""
+    c = Case(G, [700, 513, 40], [3, 1, 2], 8, G, 64, 32, dtype, nl=60)
+    run("causal", c)
+    run("window", c, 300, 20)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp4", "f32"])
 def test_split_products(dtype):
     """One sequence of many rows: its products are shared by several blocks, joined
     in order."""
