@@ -126,7 +126,7 @@ namespace {
 
 // How many splits a (layer, group, row tile)'s steps are divided into, at
 // most `most`, in a call of n sequences.
-int split_count(const AttendShape& s, int n, int d, int esz, int64_t steps, int64_t most) {
+int split_count(const AttendShape& s, int n, const PagedView& v, int64_t steps, int64_t most) {
   if (s.units == 0) return 1;
   if (!s.many) {
     // bound by HBM: splits of at least two steps for each of a block's waves
@@ -137,8 +137,11 @@ int split_count(const AttendShape& s, int n, int d, int esz, int64_t steps, int6
     // and of so many blocks in all that each CU has two, which keep HBM busy.
     // 512 against 1,024 blocks: 28 layers of 4 trees of 4 tokens 126 and 148
     // us, 64 sequences of one token 85 and 92, float32 trees of up to 13 tokens
-    // 37 and 40; 12 sequences of 3,000 to 9,000 tokens 62 and 54
-    const int64_t blocks = 512;
+    // 37 and 40; 12 sequences of 3,000 to 9,000 tokens 62 and 54.  Rows of 32
+    // bytes (4 bits, 64 elements) have twice as many, whose starts are more of
+    // their time: 16 sequences of 500 to 13,711 tokens, one token 24.3 and 22.5,
+    // trees of seven 29.2 and 26.6
+    const int64_t blocks = v.row == 32 ? 1024 : 512;
     // of several sequences, whose lengths may be far from each other, none of
     // over 3,200 tokens (float32: 1,536), or one long sequence would hold up
     // the rest (two layers of 18 trees of 3 tokens over 215 to 30,867 140 us
@@ -146,7 +149,7 @@ int split_count(const AttendShape& s, int n, int d, int esz, int64_t steps, int6
     // 442 and 355), as far as 4,096 blocks go: the bound on the lengths may be
     // a whole table row, of which little is in use, and every split has its
     // place in the workspace
-    const int64_t longest = esz == 2 ? 100 : 48;
+    const int64_t longest = v.esz == 2 ? 100 : 48;
     const int64_t even = n > 1 ? std::min((steps + longest - 1) / longest, 4096 / s.units) : 1;
     const int64_t ns = std::min((steps + least - 1) / least, std::max(even, blocks / s.units));
     return (int)std::max<int64_t>(1, std::min(ns, most));
@@ -166,7 +169,7 @@ int split_count(const AttendShape& s, int n, int d, int esz, int64_t steps, int6
   for (int64_t ns = 1; ns <= last;) {
     const int64_t per = (steps + ns - 1) / ns;
     double cost = (double)((s.units * ns + 511) / 512) * (double)(per + 4);
-    if (ns > 1) cost += 2 + (double)(s.units * ns) * s.row_tile * d * 8 / 10e6;
+    if (ns > 1) cost += 2 + (double)(s.units * ns) * s.row_tile * v.d * 8 / 10e6;
     if (ns == 1 || cost < best) {
       best = cost;
       best_ns = (int)ns;
@@ -207,12 +210,12 @@ starkv_status attend_shape(const PagedView& v, const int32_t* rows, int n, int32
   // of a call without a window, whose splits bound those of one with it.
   const int64_t len = std::min<int64_t>(max_len, v.cap);
   const int step = s->many ? 64 : 32;
-  const int most_split = split_count(*s, n, v.d, v.esz, (len + step - 1) / step, INT32_MAX);
+  const int most_split = split_count(*s, n, v, (len + step - 1) / step, INT32_MAX);
   const int64_t row_tokens = (s->row_tile + hpg - 1) / hpg + 1;
   const int64_t seen = window ? std::min<int64_t>(len, (int64_t)window + sinks + row_tokens + 2 * step)
                               : len;
   const int64_t steps = std::max<int64_t>(1, (seen + step - 1) / step);
-  s->n_split = split_count(*s, n, v.d, v.esz, steps, most_split);
+  s->n_split = split_count(*s, n, v, steps, most_split);
   s->chunk = (int)((steps + s->n_split - 1) / s->n_split * step);
   // (up to 1.6 blocks to a tile's split, each of 256 of a launch's 2^32
   // threads; and a sequence's rows stay below 2^31)
