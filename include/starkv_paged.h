@@ -282,7 +282,7 @@ starkv_status starkv_attend_window(const starkv_paged* cache, const int32_t* slo
  * starkv_attend_window, and lse what that call gave for these rows,
  *   out[t] = old[t] + sum_{i, h: t in V(i)} exp(x[h,t] - lse[i,h]),
  * old[t] = mass[t] for the tokens before the rows', 0 for the rows' own.  A row
- * whose lse is -infinity adds nothing.  All tokens of the sequence are written
+ * whose lse is -infinity or NaN adds nothing.  All tokens of the sequence are written
  * (dropped ones keep old[t]), none behind it; sequences without rows are left as
  * they are.  Logits, weights and sums are float32.
  * slots: no slot twice (E_PARAM).   rows: each at most what a table row holds,

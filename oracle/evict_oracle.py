@@ -98,7 +98,7 @@ def weights(model, slot, q, lse, see, to_f64, layer):
             if w is None:
                 continue
             k = np.repeat(to_f64(model.k[layer, w[0], :, w[1]]), H // G, axis=0)       # [H, d]
-            use = see[:, t][:, None] & (lse != -np.inf)
+            use = see[:, t][:, None] & (lse > -np.inf)         # (nor NaN)
             if not use.any():
                 continue
             x = np.einsum("thd,hd->th", q, k) / np.sqrt(d)

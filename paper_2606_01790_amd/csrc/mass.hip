@@ -175,7 +175,7 @@ struct Rows16 {
       const int row = r0 + 4 * quad + e, r = min(row, s.R - 1), qi = r / s.hpg;
       const float lse = a.lse[at + (size_t)qi * v.H + (r - qi * s.hpg)];
       l[e] = lse * kLog2e;
-      p[e] = row < s.R && lse != -INFINITY ? s.first + qi : -1;
+      p[e] = row < s.R && lse > -INFINITY ? s.first + qi : -1;      // (nor NaN)
     }
   }
   // The lane's rows' weights of token t, whose part of K the lane holds.  `whole`:
@@ -476,8 +476,8 @@ __global__ __launch_bounds__(kThreads, 2) void mass_many(PagedView v, MassArgs a
       const auto stage = [&](char* to, int buf) {
         // (before the loads into LDS: what waits for the log-sums waits for all loads before)
         if (wave == 0) {
-          // (also for the rows behind the last)
-          const bool none = lse == -INFINITY;
+          // (also for the rows behind the last, and where the sum is NaN)
+          const bool none = !(lse > -INFINITY);
           const float l = none ? INFINITY : lse * kLog2e;
           const int p = none ? -1 : s.first + li;
           ls[buf][lane] = l;

@@ -248,6 +248,19 @@ def test_rows_whose_log_sum_is_minus_infinity(T):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp4", "f32"])
 @pytest.mark.parametrize("T", [4, 40])
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+def test_rows_of_a_bad_log_sum(dtype, T, bad):
+    """They add nothing, to the tokens that they see and to the others."""
+    c = Case(16, [130, T + 1], [T, T], 8, 2, 64, 16, dtype)
+    for window, sinks in ((0, 0), (20, 3)):
+        c.upload(window, sinks)
+        c.lse[0, 1, 3] = c.lse[0, T + 2, :] = bad
+        c.call(window, sinks)
+        c.check(f"bad rows {window}", window, sinks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp4", "f32"])
+@pytest.mark.parametrize("T", [4, 40])
 def test_infinities_and_nan(dtype, T):
     """In K: they spoil the masses of their own tokens where rows see them, and no
     others."""
