@@ -74,8 +74,8 @@ extern "C" {
  * when the call began, in the order of the call's sequences; they look for
  * them from page 0 up, 4 us for every 8,192 pages before the last that they
  * take.  To write or attend to one layer of a cache, pass n_layers = 1 and k, v
- * moved on by the layer's offset; grow and compact move rows of the layers that
- * they are given and change the table once, so they take all layers. */
+ * moved on by the layer's offset; grow, compact and evict move rows of the layers
+ * that they are given and change the table once, so they take all layers. */
 typedef struct starkv_paged {
   int32_t n_layers;
   int32_t H;
@@ -275,7 +275,11 @@ starkv_status starkv_attend_window(const starkv_paged* cache, const int32_t* slo
  * the query tokens and heads of a layer: float32 [n_layers][n_slots][max_pages *
  * page_tokens], device, contiguous, beside the cache.  starkv_mass_add follows
  * each attention, starkv_mass_fork each fork, and starkv_pages_evict takes the
- * lightest tokens away, their masses with them. */
+ * lightest tokens away, their masses with them.  A token has a mass from the call
+ * on whose rows it is one of: it needs no start, and what lies behind a sequence
+ * or in a slot in no use is not looked at.  starkv_pages_compact moves no masses;
+ * after the compaction of a drafted tree's path, weigh the accepted tokens as rows of
+ * a starkv_attend_window call over them. */
 
 /* Add the weights of the last rows[b] >= 0 tokens (host) of each sequence: with
  * x, window, sinks and the tokens V(i) that query token i sees as for
@@ -289,7 +293,8 @@ starkv_status starkv_attend_window(const starkv_paged* cache, const int32_t* slo
  *      their sum at most 2^26 (E_PARAM).
  * q:   as for the attentions.   lse: device, float32 [n_layers][sum rows][H].
  * mass: device, as above.   out: device out, as mass; it may be mass.
- * max_len, ws: as for the attentions, with starkv_mass_workspace_bytes().
+ * max_len, ws: as for the attentions, with starkv_mass_workspace_bytes() (calls of
+ *      fewer rows or layers may need more: size it for each that is made).
  * Errors: E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_PARAM, E_WORKSPACE, E_HIP. */
 starkv_status starkv_mass_add(const starkv_paged* cache, const int32_t* slots, int32_t n,
                               const int32_t* rows, const void* q, const float* lse,

@@ -30,7 +30,10 @@
 // 28 layers 271 us (5.8 TB/s), one of each of 16 sequences of 3,000 to 12,000 116
 // (4.2); 4 trees of up to 13 tokens in 4 layers 35, 8 trees of up to 48 over
 // 1,664 to 39,197 tokens 347 (57 TFLOP/s of 154); a chunk of 1,000 tokens behind
-// 12,711 2,502 (76).
+// 12,711 2,502 (76).  4 bits: one token over 40,941 in 28 layers 120 us (624 MB, 5.2
+// TB/s), over 13,711 43, where bf16 takes 143; one of each of 32 sequences of 37 to
+// 40,941 tokens 89 (357 MB, 4.0); over 600 in one layer 11; trees of seven (28 rows
+// of 64 elements) of 16 sequences of 500 to 13,711 tokens 24.
 #include <algorithm>
 #include <type_traits>
 
@@ -155,7 +158,12 @@ __device__ inline void zero_not_finite(R& r) {
 // conversion, two at a time, as the fragments are made, and all else is the
 // same.  K's products may take the elements of a row in any order that Q's take
 // too: lane quad holds the D/4 neighbouring ones that it reads at once, which are
-// of one scale.  kOnePage: pages of 32 tokens or more, so that a step lies in one.
+// of one scale.  A step is a quarter of bf16's bytes for more instructions (219 of
+// vectors and 95 scalar ones for 32 tokens), so its rows are asked for while the
+// step before is worked on.  (Made into bf16 only where they are used, which leaves
+// registers for a third block on a CU, they took 95 us of 32 sequences and 129 of 28
+// layers, where this takes 93 and 127.)
+// kOnePage: pages of 32 tokens or more, so that a step lies in one.
 template <typename T, int D, int NB, bool F4 = false, bool kOnePage = false>
 __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArgs a, AttendLists s,
                                                        unsigned run) {
@@ -320,21 +328,21 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
       next1 = kOnePage ? next0 : page_of(u + 2 * kWaves, 1);
     } else {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int in_page = (t0 + 16 * h) & (v.P - 1);
-      const int64_t at = base + (int64_t)page[h] * v.ps;
-      const char* kr = v.k + at + (int64_t)(in_page + l16) * v.ts + 16 * quad;
+      for (int h = 0; h < 2; ++h) {
+        const int in_page = (t0 + 16 * h) & (v.P - 1);
+        const int64_t at = base + (int64_t)page[h] * v.ps;
+        const char* kr = v.k + at + (int64_t)(in_page + l16) * v.ts + 16 * quad;
 #pragma unroll
-      for (int f = 0; f < NF; ++f) kf[h][f] = *reinterpret_cast<const frag*>(kr + 64 * f);
-      const char* vr = v.v + at + (int64_t)(in_page + 4 * quad) * v.ts + sizeof(vrow) * l16;
+        for (int f = 0; f < NF; ++f) kf[h][f] = *reinterpret_cast<const frag*>(kr + 64 * f);
+        const char* vr = v.v + at + (int64_t)(in_page + 4 * quad) * v.ts + sizeof(vrow) * l16;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int c = 0; c < VR::kLoads; ++c)
-          vv[4 * h + j][c] = *reinterpret_cast<const vrow*>(vr + j * v.ts + 16 * sizeof(vrow) * c);
-    }
-    next0 = page_of(u + kWaves, 0);
-    next1 = page_of(u + kWaves, 1);
+          for (int c = 0; c < VR::kLoads; ++c)
+            vv[4 * h + j][c] = *reinterpret_cast<const vrow*>(vr + j * v.ts + 16 * sizeof(vrow) * c);
+      }
+      next0 = page_of(u + kWaves, 0);
+      next1 = page_of(u + kWaves, 1);
     }
     const bool whole = there[0] && there[1] && sees_step<kStep>(all, t0);
 

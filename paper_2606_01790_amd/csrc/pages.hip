@@ -283,7 +283,8 @@ __global__ __launch_bounds__(256) void write_kernel(PagedView v, Rows<N> r, Writ
 // magnitude, as an integer (which orders infinities and NaN above all numbers),
 // gives the scale by its exponent, one more where the mantissa is over 1.75; the
 // hardware's conversion divides by it, exactly, and rounds to the nearest, ties to
-// the even code.
+// the even code.  Bound by HBM (13,711 tokens in 28 layers, 786 MB read and 209
+// written: 195 us, 5.1 TB/s).
 __device__ inline uint32_t quad_max(uint32_t x) {
   x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true));   // lanes 1 0 3 2
   return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));  // lanes 2 3 0 1
@@ -316,7 +317,8 @@ __global__ __launch_bounds__(256) void write_fp4(PagedView v, Rows<N> r, WriteAr
     const int64_t rg = i / VPR;
     const int g = (int)((uint32_t)rg % (uint32_t)v.G), row = (int)((uint32_t)rg / (uint32_t)v.G);
     // the rows first, whether they are to be written or not: their way overlaps that of
-    // the page
+    // the page (the tokens above took 241 us one after the other).  They are read once,
+    // past the caches
     const int64_t from = (int64_t)layer * a.ls + (int64_t)g * a.gs + (int64_t)row * a.ts + part * 16;
     const i32x4 kk = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(a.k + from));
     const i32x4 vv = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(a.v + from));
@@ -344,7 +346,9 @@ __global__ __launch_bounds__(256) void write_fp4(PagedView v, Rows<N> r, WriteAr
 
 // The rows of tokens out of their pages, 16 bytes of K and of V per thread; of a
 // 4-bit cache the bf16 numbers that four bytes stand for.  What has no page gives
-// zeros.
+// zeros.  Bound by HBM: 13,711 tokens in 28 layers out of 4 bits 150 us (995 MB, 6.6
+// TB/s), 237 with the rows written through the caches, where they took the place of the
+// pages.
 struct ReadArgs {
   char* k;
   char* v;
