@@ -32,7 +32,7 @@ starkv_status mass_shape(const PagedView& v, const int32_t* rows, int n, int32_t
   s->n_rows = (int)tot;
   const int64_t R = most * hpg;
   // up to 32 rows of a group stay in a wave's registers while it reads K once; of more
-  // the tokens do (56 rows over 13,711 tokens in 28 layers: 115 us by tokens, and 183 with
+  // the tokens do (56 rows over 13,711 tokens in 28 layers: 100 us by tokens, and 183 with
   // four blocks of 16 rows in registers)
   s->many = R > 32;
   s->row_blocks = (int)std::max<int64_t>(1, (R + 15) / 16);
@@ -54,17 +54,19 @@ starkv_status mass_shape(const PagedView& v, const int32_t* rows, int n, int32_t
   s->tile = 256;
   s->tiles = (int)((len + s->tile - 1) / s->tile);
   s->blocks = (int)std::max<int64_t>(1, std::min<int64_t>(s->tiles, (1 << 22) / pairs));
-  // splits of a tile's (group, 32 rows) products until there are 2,048 blocks, of
-  // at least four products (100 rows over 100 tokens: 33 us with at least 16, and 20
-  // so); a multiple of the 8 XCDs, each of which then reads the
-  // same eighth of Q for every tile (2,755 rows over 13,711 tokens: 32, 40 or 48
-  // splits 287 us, 37 298, 16 290, 9 310)
-  const int64_t products = v.G * ((R + 31) / 32);
-  s->n_split = (int)std::max<int64_t>(
-      1, std::min({2048 / (pairs * s->tiles), products / 4, (int64_t)64}));
+  // splits of a tile's (group, 32 rows) products until there are 2,048 blocks, of at
+  // least four products (100 rows over 100 tokens: 33 us with at least 16, and 20 so),
+  // or 4,096 of at least 16, whose last round is shorter (40 rows of 4 sequences of 1,000
+  // to 4,000 tokens in 28 layers 207 and 188 us; but 8 rows over 13,711, of which it
+  // would leave four products, 100 and 109); a multiple of the 8 XCDs, each of which then
+  // reads the same eighth of Q for every tile (2,755 rows over 13,711 tokens: 32, 40 or
+  // 48 splits 287 us, 37 298, 16 290, 9 310)
+  const int64_t products = v.G * ((R + 31) / 32), units = pairs * s->tiles;
+  s->n_split = (int)std::clamp<int64_t>(
+      std::max(std::min(2048 / units, products / 4), std::min(4096 / units, products / 16)), 1, 64);
   if (s->n_split > 8) s->n_split &= ~7;
   if (s->n_split > 1)
-    s->ws_bytes = (size_t)pairs * s->n_split * s->tiles * s->tile * sizeof(float);
+    s->ws_bytes = (size_t)units * s->n_split * s->tile * sizeof(float);
   return STARKV_OK;
 }
 

@@ -20,8 +20,8 @@
 // in one layer 125 in bf16 (5.5), 53 in 4 bits, 242 in float32; one over 13,711 in 28
 // layers 74, 33 and 143, four 85, 44 and 201.  4 bits are bound by what the waves issue.
 // Many rows, with the join (5 us): 2,755 over 13,711 tokens 276 us (244 GFLOP, 880
-// TFLOP/s), in 4 bits 278, in float32 2,350 (104; a library product makes 154); all of
-// 8,192 353 (680); 16 rows over 13,711 in 28 layers 145, 99 and 495.  The matrix units
+// TFLOP/s), in 4 bits 260, in float32 2,330 (104; a library product makes 154); all of
+// 8,192 335 (720); 16 rows over 13,711 in 28 layers 125, 93 and 490.  The matrix units
 // are busy in 40% of the SIMDs' cycles, as in the attention of many rows, and for the
 // same reason: 8.7 vector instructions to a product.
 #include <algorithm>
@@ -436,37 +436,28 @@ __global__ __launch_bounds__(kThreads, 2) void mass_many(PagedView v, MassArgs a
   // x / hpg is the upper half of x * per_head for x < 2^20 (hpg is under 2^12)
   const uint32_t per_head = (uint32_t)(((1ull << 32) + s.hpg - 1) / s.hpg);
 
-  for (int tile = at % a.blocks; (int64_t)tile * kTile < s.n; tile += a.blocks) {
+  // (the first tile moves on with the sequence and the layer: the XCDs take the blocks by
+  // turns, and those of the last tiles, which short sequences do not have, are spread over
+  // them; 40 rows of 4 sequences in 28 layers 240 -> 207 us)
+  for (int tile = (at % a.blocks + b + layer) % a.blocks; (int64_t)tile * kTile < s.n; tile += a.blocks) {
     Share share;
     if (!share.take(v, a, s, tile, split)) continue;
     const int t0 = share.t0;
     float sum[2][2] = {};
+    // K of the wave's tokens: a lane holds half a row of tokens l32 and 32 + l32
+    const char* rows_of[2];           // in group 0's block
+    const char* scales_of[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int t = min(t0 + 64 * wave + 32 * h + l32, s.n - 1);
+      const int page = table_of(v, s)[t >> v.psh], in_page = t & (v.P - 1);
+      const char* block = v.k + (int64_t)layer * v.ls + (int64_t)(is_page(v, page) ? page : 0) * v.ps;
+      rows_of[h] = block + (int64_t)in_page * v.ts + half * (F4 ? D / 4 : kRow / 2);
+      scales_of[h] = block + v.P * (D / 2) + in_page * (D / 32) + half * (D / 64);
+    }
     int g, from, to;
     while (share.next(&g, &from, &to)) {
-      // K of the wave's tokens: a lane holds half a row of tokens l32 and 32 + l32
       bf16x8 kf[2][NF];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int t = min(t0 + 64 * wave + 32 * h + l32, s.n - 1);
-        const int page = table_of(v, s)[t >> v.psh], in_page = t & (v.P - 1);
-        const char* block = v.k + (int64_t)layer * v.ls + (int64_t)(is_page(v, page) ? page : 0) * v.ps +
-                            (int64_t)g * v.gs;
-        if constexpr (F4) {
-          const char* row = block + in_page * (D / 2) + half * (D / 4);
-          const char* scales = block + v.P * (D / 2) + in_page * (D / 32) + half * (D / 64);
-#pragma unroll
-          for (int f = 0; f < NF; f += 4) {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(row + 4 * f);
-            const float sc = __uint_as_float((uint32_t)*reinterpret_cast<const uint8_t*>(scales + f / 4) << 23);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) kf[h][f + e] = from_fp4(w[e], sc);
-          }
-        } else {
-          const char* row = block + (int64_t)in_page * v.ts + half * (kRow / 2);
-#pragma unroll
-          for (int f = 0; f < NF; ++f) kf[h][f] = *reinterpret_cast<const bf16x8*>(row + 16 * f);
-        }
-      }
       // Rows 32*from.. in stages of 64, asked for in order: query token i0 and head h0
       // are the stage's first row, and row x behind it is head (h0 + x) % hpg of token
       // i0 + (h0 + x) / hpg; rows behind the last repeat it.  A thread's pieces are of
@@ -477,35 +468,39 @@ __global__ __launch_bounds__(kThreads, 2) void mass_many(PagedView v, MassArgs a
       static_assert(q_swizzle<D>(kLoadRows) == 0, "whole turns of the swizzle");
       int first = 32 * from, i0 = first / s.hpg, h0 = first - i0 * s.hpg;
       const int ahead_i = kStage / s.hpg, ahead_h = kStage - ahead_i * s.hpg;
-      // of wave 0's lanes: a row's log-sum, read a stage ahead, and its query token
+      // of wave 0's lanes: a row's query token, and its log-sum, read a stage ahead
       int lrow = 32 * from + lane, li = lrow / s.hpg, lhead = lrow - li * s.hpg;
-      const auto log_sum = [&]() {
-        return lrow < s.R ? a.lse[group_at + (size_t)li * v.H + lhead] : -INFINITY;
-      };
-      float lse = wave == 0 ? log_sum() : 0.f;
-      const auto stage = [&](char* to, int buf) {
-        // (before the loads into LDS: what waits for the log-sums waits for all loads before)
-        if (wave == 0) {
-          // (also for the rows behind the last, and where the sum is NaN)
-          const bool none = !(lse > -INFINITY);
-          const float l = none ? INFINITY : lse * kLog2e;
-          const int p = none ? -1 : s.first + li;
-          ls[buf][lane] = l;
-          ps[buf][lane] = p;
-          // positions rise with the rows: the first and the last of each 32, or -1
-          // where one sees nothing
-          const uint64_t dead = __ballot(p < 0);
-          if (l32 == 0) span[buf][half][0] = (uint32_t)(dead >> (32 * half)) ? -1 : p;
-          if (l32 == 31) span[buf][half][1] = p;
-          lrow += kStage;
-          li += ahead_i;
-          lhead += ahead_h;
-          if (lhead >= s.hpg) {
-            lhead -= s.hpg;
-            ++li;
+      const auto log_sum = [&](int more) {        // of `more` stages behind
+        const int row = lrow + more * kStage;
+        int i = li + more * ahead_i, head = lhead + more * ahead_h;
+        for (int j = 0; j < more; ++j)
+          if (head >= s.hpg) {
+            head -= s.hpg;
+            ++i;
           }
-          lse = log_sum();
+        return row < s.R ? a.lse[group_at + (size_t)i * v.H + head] : -INFINITY;
+      };
+      const auto put_sums = [&](int buf, float lse) {
+        // (also for the rows behind the last, and where the sum is NaN)
+        const bool none = !(lse > -INFINITY);
+        const float l = none ? INFINITY : lse * kLog2e;
+        const int p = none ? -1 : s.first + li;
+        ls[buf][lane] = l;
+        ps[buf][lane] = p;
+        // positions rise with the rows: the first and the last of each 32, or -1
+        // where one sees nothing
+        const uint64_t dead = __ballot(p < 0);
+        if (l32 == 0) span[buf][half][0] = (uint32_t)(dead >> (32 * half)) ? -1 : p;
+        if (l32 == 31) span[buf][half][1] = p;
+        lrow += kStage;
+        li += ahead_i;
+        lhead += ahead_h;
+        if (lhead >= s.hpg) {
+          lhead -= s.hpg;
+          ++li;
         }
+      };
+      const auto load_rows = [&](char* to) {
         const char* const at = a.q + (group_at + (size_t)i0 * v.H) * kRow;
         const int last = h0 + s.R - 1 - first;
 #pragma unroll
@@ -573,9 +568,45 @@ __global__ __launch_bounds__(kThreads, 2) void mass_many(PagedView v, MassArgs a
         __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
         __syncthreads();
       };
+      // (all loads at once: the first two stages' rows and log-sums, and K)
       __syncthreads();                        // the rows before are done with
-      stage(q0, 0);
-      if (rows > 2) stage(q1, 1);
+      load_rows(q0);
+      if (rows > 2) load_rows(q1);
+      float lse = 0.f, lse0 = 0.f, lse1 = 0.f;
+      if (wave == 0) {
+        lse0 = log_sum(0);
+        lse1 = log_sum(1);
+        lse = log_sum(2);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const char* row = rows_of[h] + (int64_t)g * v.gs;
+        if constexpr (F4) {
+          const char* scales = scales_of[h] + (int64_t)g * v.gs;
+#pragma unroll
+          for (int f = 0; f < NF; f += 4) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(row + 4 * f);
+            const float sc = __uint_as_float((uint32_t)*reinterpret_cast<const uint8_t*>(scales + f / 4) << 23);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) kf[h][f + e] = from_fp4(w[e], sc);
+          }
+        } else {
+#pragma unroll
+          for (int f = 0; f < NF; ++f) kf[h][f] = *reinterpret_cast<const bf16x8*>(row + 16 * f);
+        }
+      }
+      if (wave == 0) {
+        put_sums(0, lse0);
+        put_sums(1, lse1);
+      }
+      const auto stage = [&](char* to, int buf) {
+        // (before the loads into LDS: what waits for the log-sums waits for all loads before)
+        if (wave == 0) {
+          put_sums(buf, lse);
+          lse = log_sum(0);
+        }
+        load_rows(to);
+      };
       landed();
 #pragma unroll
       for (int f = 0; f < NF; ++f)
@@ -619,7 +650,7 @@ __global__ __launch_bounds__(kThreads, 2) void mass_many_f32(PagedView v, MassAr
   const int pair = at / a.blocks, b = pair % r.n, layer = pair / r.n;
   const Seq s = seq_of(v, r, layer, b);
   if (s.T == 0) return;
-  for (int tile = at % a.blocks; (int64_t)tile * kTile < s.n; tile += a.blocks) {
+  for (int tile = (at % a.blocks + b + layer) % a.blocks; (int64_t)tile * kTile < s.n; tile += a.blocks) {
     Share share;
     if (!share.take(v, a, s, tile, split)) continue;
     const int tw = share.t0 + 64 * wave, te = min(tw + 64, s.n);      // the wave's tokens

@@ -132,7 +132,7 @@ int main() {
       if (s.many) {
         CHECK(s.tile == 256 && s.blocks <= s.tiles && pairs * s.blocks * s.n_split <= 1 << 22);
         CHECK(s.n_split <= 64 && (s.n_split < 8 || s.n_split % 8 == 0));
-        CHECK(s.n_split == 1 || pairs * s.tiles * s.n_split <= 2048);
+        CHECK(s.n_split == 1 || pairs * s.tiles * s.n_split <= 4096);
         CHECK(s.ws_bytes == (s.n_split > 1 ? (size_t)pairs * s.n_split * s.tiles * 256 * 4 : 0));
         split += s.n_split > 1;
       } else {
