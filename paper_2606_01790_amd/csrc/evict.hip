@@ -13,7 +13,9 @@
 // Bound by that chain, not by the bytes: two sequences of 10,956 and 13,711 tokens in
 // 28 layers (56 blocks) 21 us, and 34 before one wave took the last rounds and lanes
 // counted their own keys; 16 sequences of up to 1,500 in one layer 10.  The rows' moves
-// cost 110 and 6.
+// cost 110 and 6.  Above 32,768 tokens half of the keys lie in LDS (40,941 in 28 layers 61
+// us, and about 250 with all keys read again each round), above 65,536 they are read
+// again for every two bits (131,072 in one layer 322).
 #include <algorithm>
 
 #include "device_common.h"
@@ -69,42 +71,69 @@ __device__ inline uint32_t key_of(const PagedView& v, int page, float m, int t, 
   return t < sinks ? kSink : m != m ? kNan : fkey(m + 0.f);      // (-0 counts as 0)
 }
 
-// The keys and masses of a wave's tokens [first, first + 64 * count): in N registers a
-// lane, or (N = 0) read again each time.
+// The mass that a key below kNan is of (0 for -0).
+__device__ inline float mass_of(uint32_t key) {
+  return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+
+// The keys of a wave's tokens [first, first + 64 * count): N to a lane, in registers with
+// their masses, or the first 32 in registers and the rest in LDS; or (N = 0) read again each time.
+constexpr int kRegs = 32;
 template <int N>
 struct Keys {
-  uint32_t k[N > 0 ? N : 1];
-  float m[N > 0 ? N : 1];
+  static constexpr int kHere = N > kRegs ? kRegs : N;
+  static constexpr int kLoads = N > 0 && N <= kRegs ? N : 16;      // at once
+  uint32_t k[N > 0 ? kHere : 1];
+  static constexpr bool kMasses = N > 0 && N <= kRegs;
+  float m[kMasses ? N : 1];
+  uint32_t* more;                  // [N - kRegs][kThreads]
   const PagedView& v;
   const int32_t* table;
   const float* mass;
   int first, count, span, sinks;
 
   __device__ inline int token(int j) const { return first + 64 * j + (int)(threadIdx.x & 63); }
-  __device__ inline void load() {
-    // all loads at once: those behind the last token are of the last
-    int page[N > 0 ? N : 1];
+  // f(key, mass, j) from j0 on, all loads at once: those behind the last token are of the
+  // last, and their keys 0
+  template <typename F>
+  __device__ inline void read(int j0, F f) const {
+    int page[kLoads];
+    float x[kLoads];
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int t = min(token(j), span - 1);
-      m[j] = mass[t];
+    for (int j = 0; j < kLoads; ++j) {
+      const int t = min(token(j0 + j), span - 1);
+      x[j] = mass[t];
       page[j] = table[t >> v.psh];
     }
 #pragma unroll
-    for (int j = 0; j < N; ++j) k[j] = j < count ? key_of(v, page[j], m[j], token(j), span, sinks) : 0;
+    for (int j = 0; j < kLoads; ++j)
+      f(j0 + j < count ? key_of(v, page[j], x[j], token(j0 + j), span, sinks) : 0, x[j], j0 + j);
   }
+  __device__ inline void load() {
+#pragma unroll
+    for (int j0 = 0; j0 < N; j0 += kLoads)
+      read(j0, [&](uint32_t key, float x, int j) {
+        if (j < kHere) k[j] = key;
+        else more[(j - kRegs) * kThreads + threadIdx.x] = key;
+        if constexpr (kMasses) m[j] = x;
+      });
+  }
+  __device__ inline float mass_at(uint32_t key, int j) const { return key < kNan ? mass_of(key) : mass[token(j)]; }
   // f(key, mass, j) for each of them, in the order of the tokens
   template <typename F>
   __device__ inline void each(F f) const {
     if constexpr (N > 0) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) f(k[j], m[j], j);        // (those behind the last are 0)
-    } else {
-      for (int j = 0; j < count; ++j) {
-        const int t = min(token(j), span - 1);
-        const float x = mass[t];
-        f(key_of(v, table[t >> v.psh], x, token(j), span, sinks), x, j);
+      for (int j = 0; j < kHere; ++j) f(k[j], kMasses ? m[j] : mass_at(k[j], j), j);   // (those behind the last are 0)
+      if constexpr (N > kRegs) {
+#pragma unroll 8
+        for (int j = kRegs; j < N; ++j) {
+          const uint32_t x = more[(j - kRegs) * kThreads + threadIdx.x];
+          f(x, mass_at(x, j), j);
+        }
       }
+    } else {
+      for (int j0 = 0; j0 < count; j0 += kLoads) read(j0, f);
     }
   }
   // How many there are of at least `bound`, in all lanes: each lane counts its own
@@ -113,6 +142,16 @@ struct Keys {
     int c = 0;
     each([&](uint32_t x, float, int) { c += x >= bound; });
     return wave_sum(c);
+  }
+  // The same for three bounds, in one pass.
+  __device__ inline void at_least(const uint32_t (&bound)[3], int (&c)[3]) const {
+    c[0] = c[1] = c[2] = 0;
+    each([&](uint32_t x, float, int) {
+#pragma unroll
+      for (int i = 0; i < 3; ++i) c[i] += x >= bound[i];
+    });
+#pragma unroll
+    for (int i = 0; i < 3; ++i) c[i] = wave_sum(c[i]);
   }
 };
 
@@ -159,23 +198,37 @@ struct Search {
 constexpr int kCands = 1024;
 
 template <int N>
-__device__ void select(const PagedView& v, const EvictArgs& a, int b, int layer, int n_seqs,
-                       int slot, int n, Counts* sh, uint32_t* cands) {
+__device__ __forceinline__ void select(const PagedView& v, const EvictArgs& a, int b, int layer,
+                                       int n_seqs, int slot, int n, Counts* sh, uint32_t* cands,
+                                       uint32_t* more) {
   const int want = a.sinks + a.keep, span = n - a.recent;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int per = (span + kThreads - 1) / kThreads;          // groups of 64 tokens of a wave
   const float* mass = mass_row(v, a.mass, layer, slot);
-  Keys<N> keys{{}, {}, v, v.table + (size_t)slot * v.max_pages, mass, w * per * 64, per, span, a.sinks};
+  Keys<N> keys{{}, {}, more, v, v.table + (size_t)slot * v.max_pages, mass, w * per * 64, per, span, a.sinks};
   keys.load();
   int turn = 0;
-  Totals t = block_totals(sh[turn++ & 1], keys.at_least(1), keys.at_least(kSink));
+  int some[3];
+  keys.at_least({1, kSink, kSink}, some);
+  Totals t = block_totals(sh[turn++ & 1], some[0], some[1]);
   const int here = t.a, K = here - t.b <= a.keep ? here : t.b + a.keep;
   Search f{K, 0, here};
   if (K == here) {
     f.T = 1;
   } else {
-    while (!f.done() && f.met - f.over > kCands)
-      f.settle(block_totals(sh[turn++ & 1], keys.at_least(f.next())).a);
+    while (!f.done() && f.met - f.over > kCands) {
+      if (N > 0 || f.bit == 0) {
+        f.settle(block_totals(sh[turn++ & 1], keys.at_least(f.next())).a);
+      } else {
+        // two bits of a pass over keys that are read again
+        const uint32_t half = 1u << (f.bit - 1);
+        int c[3];
+        keys.at_least({f.T | half, f.T | 2 * half, f.T | 3 * half}, c);
+        const Totals lo = block_totals(sh[turn++ & 1], c[0], c[1]), hi = block_totals(sh[turn++ & 1], c[2]);
+        f.settle(lo.b);
+        if (!f.done()) f.settle(lo.b >= K ? hi.a : lo.a);
+      }
+    }
     if (!f.done()) {
       const uint32_t mask = f.bit == 31 ? 0u : ~0u << (f.bit + 1);
       const auto agrees = [&](uint32_t x) { return x != 0 && (x & mask) == f.T; };
@@ -209,8 +262,9 @@ __device__ void select(const PagedView& v, const EvictArgs& a, int b, int layer,
   }
   const uint32_t T = f.T;
   // all above T, and of those at T the first ones
-  const int above = T == kSink ? 0 : keys.at_least(T + 1), level = keys.at_least(T) - above;
-  t = block_totals(sh[turn++ & 1], above, level);
+  keys.at_least({T, T + (T != kSink), kSink}, some);
+  const int above = T == kSink ? 0 : some[1];
+  t = block_totals(sh[turn++ & 1], above, some[0] - above);
   const int most = K - t.a;
   int seen = t.before(t.mine.y), pos = t.before(t.mine.x) + min(seen, most);
   const size_t row = (size_t)layer * n_seqs + b;
@@ -241,6 +295,7 @@ __device__ void select(const PagedView& v, const EvictArgs& a, int b, int layer,
 __global__ __launch_bounds__(kThreads) void evict_select(PagedView v, Slots s, EvictArgs a) {
   __shared__ Counts sh[2];
   __shared__ uint32_t cands[kCands];
+  __shared__ uint32_t more[kRegs * kThreads];       // (a CU holds one block, by its registers)
   const int b = blockIdx.x % s.n, layer = blockIdx.x / s.n, slot = s.slot[b];
   const int n = seq_len(v, slot);
   const int want = a.sinks + a.keep;
@@ -254,10 +309,11 @@ __global__ __launch_bounds__(kThreads) void evict_select(PagedView v, Slots s, E
     return;
   }
   const int span = n - a.recent;
-  if (span <= 4 * kThreads) select<4>(v, a, b, layer, s.n, slot, n, sh, cands);
-  else if (span <= 16 * kThreads) select<16>(v, a, b, layer, s.n, slot, n, sh, cands);
-  else if (span <= 32 * kThreads) select<32>(v, a, b, layer, s.n, slot, n, sh, cands);
-  else select<0>(v, a, b, layer, s.n, slot, n, sh, cands);
+  if (span <= 4 * kThreads) select<4>(v, a, b, layer, s.n, slot, n, sh, cands, more);
+  else if (span <= 16 * kThreads) select<16>(v, a, b, layer, s.n, slot, n, sh, cands, more);
+  else if (span <= 32 * kThreads) select<32>(v, a, b, layer, s.n, slot, n, sh, cands, more);
+  else if (span <= 64 * kThreads) select<64>(v, a, b, layer, s.n, slot, n, sh, cands, more);
+  else select<0>(v, a, b, layer, s.n, slot, n, sh, cands, more);
 }
 
 // Masses of a forked sequence, a row of blocks to a (layer, sequence): 24,667 tokens'

@@ -122,6 +122,20 @@ def test_long_sequences(n):
     b.evict(b.slots, n // 5, 4, 32)
 
 
+@pytest.mark.parametrize("n", [20000, 33000, 34000, 66000])
+def test_long_sequences_of_odd_masses(n):
+    """Ties over many waves, numbers of any bits, tokens without a page, little and
+    nearly all kept."""
+    masses = {"few": lambda r, s: r.integers(0, 3, s), "equal": lambda r, s: np.ones(s),
+              "bits": lambda r, s: r.integers(0, 1 << 32, s).astype(np.uint32).view(np.float32),
+              "close": lambda r, s: (np.float32(0.7).view(np.int32) + r.integers(0, 40, s)).astype(np.int32).view(np.float32)}
+    for name, f in masses.items():
+        for keep, sinks in ((7, 0), (n // 2, 70), (n - 400, 3)):
+            b = Both(keep, [n], nl=1, G=1, P=256, spare=n // 256 + 4, masses=f)
+            b.m._let_go(b.slots[0], [1, 20, 77])
+            b.upload().evict(b.slots, keep, sinks, 32, name)
+
+
 def test_equal_and_odd_masses():
     """Ties go to the lowest token; zeros of both signs are equal; infinities; NaN
     counts as the largest."""
