@@ -17,8 +17,8 @@
 //
 // Measured, few rows: one token of each of 16 sequences of 500 to 2,747 tokens in 28
 // layers 137 us (754 MB, 5.5 TB/s; a copy makes 4.9), of 32 sequences of 37 to 40,941
-// in one layer 125 in bf16 (5.5), 53 in 4 bits, 242 in float32; one over 13,711 in 28
-// layers 74, 33 and 143, four 85, 44 and 201.  4 bits are bound by what the waves issue.
+// in one layer 125 in bf16 (5.5), 43 in 4 bits, 242 in float32; one over 13,711 in 28
+// layers 74, 26 and 143, four 85, 40 and 201.  4 bits are bound by what the waves issue.
 // Many rows, with the join (5 us): 2,755 over 13,711 tokens 276 us (244 GFLOP, 880
 // TFLOP/s), in 4 bits 260, in float32 2,330 (104; a library product makes 154); all of
 // 8,192 335 (720); 16 rows over 13,711 in 28 layers 125, 93 and 490.  The matrix units
@@ -265,16 +265,16 @@ struct Tiles {
   }
 };
 
-// A block takes tiles of S parts of a group (a part is 16 tokens, 32 in 4 bits, whose rows
-// are shorter), and of all groups' parts each wave a quarter, whole groups first.  The next part's K is on its way while one is worked
+// A block takes tiles of S parts of a group (a part is 16 tokens, 64 in 4 bits: as many
+// bytes on their way; with 32, 28 layers of 40,941 tokens took 99 us and not 79), and of all groups' parts each wave a quarter, whole groups first.  The next part's K is on its way while one is worked
 // on, across tiles.  NB: the 16-row blocks of every sequence, which stay in registers
 // while the group does.
-template <typename T, int D, int NB>      // blocks of a CU
-constexpr int kResident = sizeof(T) == 4 && D == 128 ? (NB == 2 ? 2 : 3) : NB == 1 ? 5 : 4;
+template <typename T, int D, bool F4, int NB>      // blocks of a CU
+constexpr int kResident = sizeof(T) == 4 && D == 128 ? (NB == 2 ? 2 : 3) : (NB == 1 ? 5 : 4) - (F4 && D == 128);
 template <bool F4>
-constexpr int kPart = F4 ? 32 : 16;
+constexpr int kPart = F4 ? 64 : 16;
 template <typename T, int D, bool F4, int NB, int S>
-__global__ __launch_bounds__(kThreads, (kResident<T, D, NB>)) void mass_few(PagedView v, MassArgs a,
+__global__ __launch_bounds__(kThreads, (kResident<T, D, F4, NB>)) void mass_few(PagedView v, MassArgs a,
                                                                           RowList r) {
   constexpr int kTokens = S * kPart<F4>, kHalves = kPart<F4> / 16;
   struct K {
@@ -747,11 +747,11 @@ int launch_mass_add(const PagedView& v, const MassCall& c, void* stream) {
     using T = typename decltype(t)::type;
     constexpr int D = decltype(d)::value, NB = decltype(nb)::value;
     constexpr bool F4 = decltype(f4)::value;
-    const unsigned blocks = (unsigned)std::min<int64_t>(c.s.blocks, 256 * kResident<T, D, NB>);
+    const unsigned blocks = (unsigned)std::min<int64_t>(c.s.blocks, 256 * kResident<T, D, F4, NB>);
     const auto go = [&](auto kernel) { kernel<<<blocks, kThreads, lds, st>>>(v, a, c.r); };
     if (c.s.tile == kPart<F4>) go(mass_few<T, D, F4, NB, 1>);
     else if (c.s.tile == 4 * kPart<F4>) go(mass_few<T, D, F4, NB, 4>);
-    else go(mass_few<T, D, F4, NB, kThreads / kPart<F4>>);
+    else if constexpr (!F4) go(mass_few<T, D, F4, NB, kThreads / kPart<F4>>);
   };
   const auto by_rows = [&](auto t, auto d, auto f4) {
     using T = typename decltype(t)::type;
