@@ -265,18 +265,19 @@ struct Tiles {
   }
 };
 
-// A block takes tiles of S parts of a group (a part is 16 tokens, 64 in 4 bits: as many
-// bytes on their way; with 32, 28 layers of 40,941 tokens took 99 us and not 79), and of all groups' parts each wave a quarter, whole groups first.  The next part's K is on its way while one is worked
-// on, across tiles.  NB: the 16-row blocks of every sequence, which stay in registers
-// while the group does.
+// A block takes tiles of S parts of a group, and of all groups' parts each wave a
+// quarter, whole groups first.  The next part's K is on its way while one is worked on,
+// across tiles: a part is 4 KB of K, 16 tokens of 256 bytes, or 64 tokens (in 4 bits, with
+// 32, 28 layers of 40,941 tokens took 99 us and not 79).  NB: the 16-row blocks of every
+// sequence, which stay in registers while the group does.
 template <typename T, int D, bool F4, int NB>      // blocks of a CU
 constexpr int kResident = sizeof(T) == 4 && D == 128 ? (NB == 2 ? 2 : 3) : (NB == 1 ? 5 : 4) - (F4 && D == 128);
-template <bool F4>
-constexpr int kPart = F4 ? 64 : 16;
+template <typename T, int D, bool F4>
+constexpr int kPart = F4 ? 64 : sizeof(T) * D == 128 ? 32 : 16;
 template <typename T, int D, bool F4, int NB, int S>
 __global__ __launch_bounds__(kThreads, (kResident<T, D, F4, NB>)) void mass_few(PagedView v, MassArgs a,
                                                                           RowList r) {
-  constexpr int kTokens = S * kPart<F4>, kHalves = kPart<F4> / 16;
+  constexpr int kTokens = S * kPart<T, D, F4>, kHalves = kPart<T, D, F4> / 16;
   struct K {
     KRow<T, D, F4> half[kHalves];
   };
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(kThreads, (kResident<T, D, F4, NB>)) void mass_few(
     const int g = p / S;
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
-      const int t = min(first + kPart<F4> * (p % S) + 16 * h, (q.n - 1) & ~15);
+      const int t = min(first + kPart<T, D, F4> * (p % S) + 16 * h, (q.n - 1) & ~15);
       const int page = const_ints(table_of(v, q))[t >> v.psh];
       // where there is no page the products are of page 0's, and dropped
       k.half[h].load(v, v.k + (int64_t)q.layer * v.ls + (int64_t)(is_page(v, page) ? page : 0) * v.ps +
@@ -327,7 +328,7 @@ __global__ __launch_bounds__(kThreads, (kResident<T, D, F4, NB>)) void mass_few(
     if (part < p1) {
 #pragma unroll
       for (int h = 0; h < kHalves; ++h) {
-        const int in_tile = kPart<F4> * (part % S) + 16 * h + l16, t = t0 + in_tile;
+        const int in_tile = kPart<T, D, F4> * (part % S) + 16 * h + l16, t = t0 + in_tile;
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < NB; ++i) sum += rows[i].weigh(a, k.half[h], t, whole);
@@ -749,12 +750,11 @@ int launch_mass_add(const PagedView& v, const MassCall& c, void* stream) {
     constexpr bool F4 = decltype(f4)::value;
     const unsigned blocks = (unsigned)std::min<int64_t>(c.s.blocks, 256 * kResident<T, D, F4, NB>);
     const auto go = [&](auto kernel) { kernel<<<blocks, kThreads, lds, st>>>(v, a, c.r); };
-    if (c.s.tile == kPart<F4>) go(mass_few<T, D, F4, NB, 1>);
-    else if (c.s.tile == 4 * kPart<F4>) go(mass_few<T, D, F4, NB, 4>);
-    else if constexpr (!F4) go(mass_few<T, D, F4, NB, kThreads / kPart<F4>>);
+    if (c.s.tile == kPart<T, D, F4>) go(mass_few<T, D, F4, NB, 1>);
+    else if (c.s.tile == 4 * kPart<T, D, F4>) go(mass_few<T, D, F4, NB, 4>);
+    else if constexpr (!F4) go(mass_few<T, D, F4, NB, kThreads / kPart<T, D, F4>>);
   };
   const auto by_rows = [&](auto t, auto d, auto f4) {
-    using T = typename decltype(t)::type;
     if (c.s.row_blocks == 1) by_tile(t, d, f4, Int<1>{});
     else by_tile(t, d, f4, Int<2>{});
   };

@@ -136,7 +136,7 @@ int main() {
         CHECK(s.ws_bytes == (s.n_split > 1 ? (size_t)pairs * s.n_split * s.tiles * 256 * 4 : 0));
         split += s.n_split > 1;
       } else {
-        const int part = v.fp4 ? 64 : 16;
+        const int part = v.fp4 ? 64 : v.row == 128 ? 32 : 16;
         CHECK((s.tile == part || s.tile == (c.G < 4 ? 256 : 4 * part)) && s.n_split == 1 && s.ws_bytes == 0);
         CHECK((int64_t)s.row_blocks * 16 >= R && s.row_blocks <= 2);
         CHECK(2 * c.G * s.tile * 4 <= 64 * 1024);       // LDS
