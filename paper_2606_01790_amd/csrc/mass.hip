@@ -267,7 +267,7 @@ struct Tiles {
 
 // A block takes tiles of S parts of a group, and of all groups' parts each wave a
 // quarter, whole groups first.  The next part's K is on its way while one is worked on,
-// across tiles: a part is 4 KB of K, 16 tokens of 256 bytes, or 64 tokens (in 4 bits, with
+// across tiles: a part is about 4 KB of K, 16, 32 or 64 tokens (in 4 bits, with
 // 32, 28 layers of 40,941 tokens took 99 us and not 79).  NB: the 16-row blocks of every
 // sequence, which stay in registers while the group does.
 template <typename T, int D, bool F4, int NB>      // blocks of a CU
