@@ -18,6 +18,7 @@
  *   starkv_attend_tree    attention of a tree of drafted tokens
  *   starkv_attend_window  attention with a sliding window and sink tokens
  *   starkv_mass_add       attention weights added up per cached token
+ *     ..._add_grown       the same behind a grow that may have found no pages
  *   starkv_mass_fork      a fork's copy of them
  *   starkv_pages_evict    the tokens of the least accumulated weight evicted
  *
@@ -288,7 +289,9 @@ starkv_status starkv_attend_window(const starkv_paged* cache, const int32_t* slo
  * old[t] = mass[t] for the tokens before the rows', 0 for the rows' own.  A row
  * whose lse is -infinity or NaN adds nothing.  All tokens of the sequence are written
  * (dropped ones keep old[t]), none behind it; sequences without rows are left as
- * they are.  Logits, weights and sums are float32.
+ * they are.  Logits, weights and sums are float32.  After a grow that left a
+ * sequence unchanged its last tokens are older ones, whose masses this call loses:
+ * behind a grow whose status the host has not read, the call below is the one.
  * slots: no slot twice (E_PARAM).   rows: each at most what a table row holds,
  *      their sum at most 2^26 (E_PARAM).
  * q:   as for the attentions.   lse: device, float32 [n_layers][sum rows][H].
@@ -301,7 +304,16 @@ starkv_status starkv_mass_add(const starkv_paged* cache, const int32_t* slots, i
                               int32_t window, int32_t sinks, int32_t max_len, const float* mass,
                               float* out, void* ws, size_t ws_bytes, void* stream);
 
-/* Bytes of device workspace of starkv_mass_add with these arguments.  0 if they
+/* The same behind the grow that made the rows: where grown[b] is not
+ * STARKV_SEQ_OK nothing is added and no token is the rows' own, out[t] = mass[t] for
+ * all tokens of the sequence.  grown: as for starkv_pages_write_grown.  Errors: as above. */
+starkv_status starkv_mass_add_grown(const starkv_paged* cache, const int32_t* slots, int32_t n,
+                                    const int32_t* rows, const void* q, const float* lse,
+                                    int32_t window, int32_t sinks, int32_t max_len,
+                                    const float* mass, float* out, const int32_t* grown, void* ws,
+                                    size_t ws_bytes, void* stream);
+
+/* Bytes of device workspace of both with these arguments.  0 if they
  * are invalid, or none is needed (ws may then be NULL). */
 size_t starkv_mass_workspace_bytes(const starkv_paged* cache, const int32_t* rows, int32_t n,
                                    int32_t max_len);

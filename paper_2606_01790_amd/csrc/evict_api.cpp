@@ -80,6 +80,41 @@ EvictWs evict_ws(const PagedView& v, int n, int64_t want, int recent) {
   return w;
 }
 
+namespace {
+
+starkv_status add(const starkv_paged* cache, const int32_t* slots, int32_t n,
+                  const int32_t* rows, const void* q, const float* lse, int32_t window,
+                  int32_t sinks, int32_t max_len, const float* mass, float* out,
+                  const int32_t* grown, void* ws, size_t ws_bytes, void* stream) {
+  PagedView v;
+  starkv_status st = check_paged(cache, &v);
+  if (st != STARKV_OK) return st;
+  if ((st = check_slots(v, slots, n, true)) != STARKV_OK) return st;
+  if (window < 0 || window > kMaxTokens || sinks < 0 || sinks > kMaxTokens) return STARKV_E_PARAM;
+  MassCall c;
+  if ((st = mass_shape(v, rows, n, max_len, &c.s)) != STARKV_OK) return st;
+  if ((st = take_rows(v, slots, rows, n, &c.r)) != STARKV_OK) return st;
+  c.r.grown = grown;
+  if (c.s.n_rows == 0) return STARKV_OK;
+  if (!q || !lse || !mass || !out) return STARKV_E_NULL;
+  if (!at(q, 16) || !at(lse, 4) || !at(mass, 4) || !at(out, 4) || !at(grown, 4))
+    return STARKV_E_ALIGN;
+  if (c.s.ws_bytes) {
+    if (!ws || ws_bytes < c.s.ws_bytes) return STARKV_E_WORKSPACE;
+    if (!at(ws, 16)) return STARKV_E_ALIGN;
+  }
+  c.q = q;
+  c.lse = lse;
+  c.mass = mass;
+  c.out = out;
+  c.part = static_cast<float*>(ws);
+  c.window = window ? window : (int32_t)kMaxTokens;
+  c.sinks = window ? sinks : 0;
+  return hip_status(launch_mass_add(v, c, stream));
+}
+
+}  // namespace
+
 }  // namespace starkv
 
 using namespace starkv;
@@ -117,29 +152,18 @@ starkv_status starkv_mass_add(const starkv_paged* cache, const int32_t* slots, i
                               const int32_t* rows, const void* q, const float* lse,
                               int32_t window, int32_t sinks, int32_t max_len, const float* mass,
                               float* out, void* ws, size_t ws_bytes, void* stream) {
-  PagedView v;
-  starkv_status st = check_paged(cache, &v);
-  if (st != STARKV_OK) return st;
-  if ((st = check_slots(v, slots, n, true)) != STARKV_OK) return st;
-  if (window < 0 || window > kMaxTokens || sinks < 0 || sinks > kMaxTokens) return STARKV_E_PARAM;
-  MassCall c;
-  if ((st = mass_shape(v, rows, n, max_len, &c.s)) != STARKV_OK) return st;
-  if ((st = take_rows(v, slots, rows, n, &c.r)) != STARKV_OK) return st;
-  if (c.s.n_rows == 0) return STARKV_OK;
-  if (!q || !lse || !mass || !out) return STARKV_E_NULL;
-  if (!at(q, 16) || !at(lse, 4) || !at(mass, 4) || !at(out, 4)) return STARKV_E_ALIGN;
-  if (c.s.ws_bytes) {
-    if (!ws || ws_bytes < c.s.ws_bytes) return STARKV_E_WORKSPACE;
-    if (!at(ws, 16)) return STARKV_E_ALIGN;
-  }
-  c.q = q;
-  c.lse = lse;
-  c.mass = mass;
-  c.out = out;
-  c.part = static_cast<float*>(ws);
-  c.window = window ? window : (int32_t)kMaxTokens;
-  c.sinks = window ? sinks : 0;
-  return hip_status(launch_mass_add(v, c, stream));
+  return add(cache, slots, n, rows, q, lse, window, sinks, max_len, mass, out, nullptr, ws,
+             ws_bytes, stream);
+}
+
+starkv_status starkv_mass_add_grown(const starkv_paged* cache, const int32_t* slots, int32_t n,
+                                    const int32_t* rows, const void* q, const float* lse,
+                                    int32_t window, int32_t sinks, int32_t max_len,
+                                    const float* mass, float* out, const int32_t* grown, void* ws,
+                                    size_t ws_bytes, void* stream) {
+  if (n > 0 && !grown) return STARKV_E_NULL;
+  return add(cache, slots, n, rows, q, lse, window, sinks, max_len, mass, out, grown, ws,
+             ws_bytes, stream);
 }
 
 starkv_status starkv_mass_fork(const starkv_paged* cache, const int32_t* src, const int32_t* dst,

@@ -51,6 +51,7 @@ struct MassArgs {
 // A sequence of the call in one layer.
 struct Seq {
   int n, T, first;          // length, query tokens, position of the first (may be negative)
+  bool kept;                // the grow before the call left it unchanged: it has no query tokens
   int row0, hpg, R;         // its first row of the call; heads, and rows, of a group
   int slot, layer;
 };
@@ -61,6 +62,8 @@ __device__ inline Seq seq_of(const PagedView& v, const RowList& r, int layer, in
   s.n = min(max(const_ints(v.len)[s.slot], 0), v.cap);
   s.row0 = r.row0[b];
   s.T = r.row0[b + 1] - s.row0;
+  s.kept = s.T > 0 && r.grown && const_ints(r.grown)[b] != STARKV_SEQ_OK;
+  if (s.kept) s.T = 0;
   s.first = s.n - s.T;
   s.hpg = v.H / v.G;
   s.R = s.T * s.hpg;
@@ -85,7 +88,7 @@ __device__ inline void store_mass(const PagedView& v, const MassArgs& a, const S
 // Whether any row sees any of the tokens [t0, t1).
 __device__ inline bool any_sees(const MassArgs& a, const Seq& s, int t0, int t1) {
   // the first row has the widest reach back; every token from it on is seen by its own row
-  return t1 - 1 > max(s.first, 0) - a.window || t0 < a.sinks;
+  return !s.kept && (t1 - 1 > max(s.first, 0) - a.window || t0 < a.sinks);
 }
 // Row position p sees token t.
 __device__ inline bool sees(const MassArgs& a, int p, int t) {
@@ -373,6 +376,14 @@ __device__ constexpr int q_swizzle(int row) {
   return D == 128 ? row & 15 : (row >> 1) & 7;
 }
 
+// The masses of a kept sequence, where they are to go elsewhere: one block's tiles.
+__device__ inline void keep_masses(const PagedView& v, const MassArgs& a, const Seq& s, int tile, int split) {
+  if (!s.kept || a.out == a.mass || split) return;
+  const size_t at = first_mass(v, s);
+  for (int64_t t = (int64_t)tile * kTile + threadIdx.x; t < s.n; t += (int64_t)a.blocks * kTile)
+    a.out[at + t] = a.mass[at + t];
+}
+
 // What a block does of a tile: `w0` to `w1` of the products of 32 rows of a group that
 // see some of it, group after group.
 struct Share {
@@ -432,7 +443,10 @@ __global__ __launch_bounds__(kThreads, 2) void mass_many(PagedView v, MassArgs a
   const int split = blockIdx.x % a.n_split, at = blockIdx.x / a.n_split;
   const int pair = at / a.blocks, b = pair % r.n, layer = pair / r.n;
   const Seq s = seq_of(v, r, layer, b);
-  if (s.T == 0) return;
+  if (s.T == 0) {
+    keep_masses(v, a, s, at % a.blocks, split);
+    return;
+  }
   const size_t row_at = ((size_t)layer * a.n_rows + s.row0) * v.H;
   // x / hpg is the upper half of x * per_head for x < 2^20 (hpg is under 2^12)
   const uint32_t per_head = (uint32_t)(((1ull << 32) + s.hpg - 1) / s.hpg);
@@ -650,7 +664,10 @@ __global__ __launch_bounds__(kThreads, 2) void mass_many_f32(PagedView v, MassAr
   const int split = blockIdx.x % a.n_split, at = blockIdx.x / a.n_split;
   const int pair = at / a.blocks, b = pair % r.n, layer = pair / r.n;
   const Seq s = seq_of(v, r, layer, b);
-  if (s.T == 0) return;
+  if (s.T == 0) {
+    keep_masses(v, a, s, at % a.blocks, split);
+    return;
+  }
   for (int tile = (at % a.blocks + b + layer) % a.blocks; (int64_t)tile * kTile < s.n; tile += a.blocks) {
     Share share;
     if (!share.take(v, a, s, tile, split)) continue;

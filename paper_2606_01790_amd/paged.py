@@ -65,6 +65,9 @@ SIGNATURES = {
                                        c_void_p]),
     "starkv_mass_add": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_int32,
                                   c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "starkv_mass_add_grown": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32,
+                                        c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
+                                        c_size_t, c_void_p]),
     "starkv_mass_workspace_bytes": (c_size_t, [_P, c_void_p, c_int32, c_int32]),
     "starkv_mass_fork": (c_int32, [_P, c_void_p, c_void_p, c_int32, c_void_p, c_void_p]),
     "starkv_pages_evict": (c_int32, [_P, c_void_p, c_int32, c_void_p, c_int32, c_int32, c_int32,
@@ -398,10 +401,12 @@ def mass_workspace_bytes(cache: Cache, rows, max_len: int) -> int:
 
 
 def mass_add(cache: Cache, slots, rows, q, lse, window: int, sinks: int, mass, out, ws,
-             max_len: int | None = None, stream=None):
+             max_len: int | None = None, stream=None, grown=None):
     """q, window, sinks: of an attend_window call, lse: what it gave.  mass, out:
     [n_layers, n_slots, tokens of a table row], of new_mass; a view of layers takes
-    the same layers of both.  out may be mass."""
+    the same layers of both.  out may be mass.  grown: the status of the pages_grow
+    of the same slots that made the rows' tokens (starkv_mass_add_grown): a sequence
+    that it left unchanged keeps its masses."""
     n, tot = len(slots), sum(rows)
     if len(rows) != n:
         raise ValueError("rows: one number per slot")
@@ -414,8 +419,13 @@ def mass_add(cache: Cache, slots, rows, q, lse, window: int, sinks: int, mass, o
     _mass(mass, cache, "mass")
     _mass(out, cache, "out")
     _buffer(ws, 0, "ws", cache.device)
-    _run("starkv_mass_add", cache, stream, _ints(slots), n, _ints(rows), _ptr(q), _ptr(lse), window,
-         sinks, cache.cap if max_len is None else max_len, _ptr(mass), _ptr(out), _ptr(ws), _bytes(ws))
+    args = (_ints(slots), n, _ints(rows), _ptr(q), _ptr(lse), window, sinks,
+            cache.cap if max_len is None else max_len, _ptr(mass), _ptr(out))
+    if grown is None:
+        _run("starkv_mass_add", cache, stream, *args, _ptr(ws), _bytes(ws))
+    else:
+        _int32(grown, n, "grown", cache.device)
+        _run("starkv_mass_add_grown", cache, stream, *args, _ptr(grown), _ptr(ws), _bytes(ws))
 
 
 def mass_fork(cache: Cache, src, dst, mass, stream=None):
