@@ -6,6 +6,14 @@
 
 namespace starkv {
 
+// Tokens of a part of a tile, which a wave of the kernel for few rows works on at a time,
+// by the bytes of a row: 4 KB of K, but 8 of float32 rows of 128 and 2 of 4-bit rows of 64
+// (4 bits with 32 tokens: 28 layers of 40,941 99 us and not 79); and the most tokens of a
+// tile, in either kernel.  A tile of few rows is one or four parts, or kMassTile, and the
+// launch refuses others.
+constexpr int mass_part(bool fp4, int row) { return fp4 ? 64 : row == 128 ? 32 : 16; }
+constexpr int kMassTile = 256;
+
 // How a call that adds weights is divided.  Few rows: `blocks` blocks take the tiles
 // of all sequences and layers in turn.  Many rows: `blocks` of each (layer,
 // sequence) take its tiles in turn, n_split of them share a tile's products, and

@@ -45,13 +45,14 @@ starkv_status mass_shape(const PagedView& v, const int32_t* rows, int n, int32_t
     // groups, so that a wave has more than one: three rows of one group, 8 sequences of
     // 13,711 tokens in 4 layers, 43 us with four parts and 30 so), or of one where those
     // are too few for the card, or the groups' sums would fill LDS
-    const int part = v.fp4 ? 64 : v.row == 128 ? 32 : 16, most = v.G < 4 ? 256 : v.fp4 && v.G > 32 ? part : 4 * part;
+    const int part = mass_part(v.fp4, v.row);
+    const int most = v.G < 4 ? kMassTile : v.fp4 && v.G > 32 ? part : 4 * part;
     s->tile = pairs * ((len + most - 1) / most) >= 512 ? most : part;
     s->tiles = (int)((len + s->tile - 1) / s->tile);
     s->blocks = (int)std::min<int64_t>(pairs * s->tiles, 1 << 20);   // (the launch takes what the card holds)
     return STARKV_OK;
   }
-  s->tile = 256;
+  s->tile = kMassTile;
   s->tiles = (int)((len + s->tile - 1) / s->tile);
   s->blocks = (int)std::max<int64_t>(1, std::min<int64_t>(s->tiles, (1 << 22) / pairs));
   // splits of a tile's (group, 32 rows) products until there are 2,048 blocks, of at

@@ -270,17 +270,17 @@ struct Tiles {
 
 // A block takes tiles of S parts of a group, and of all groups' parts each wave a
 // quarter, whole groups first.  The next part's K is on its way while one is worked on,
-// across tiles: a part is about 4 KB of K, 16, 32 or 64 tokens (in 4 bits, with
-// 32, 28 layers of 40,941 tokens took 99 us and not 79).  NB: the 16-row blocks of every
-// sequence, which stay in registers while the group does.
+// across tiles.  NB: the 16-row blocks of every sequence, which stay in registers while
+// the group does.
 template <typename T, int D, bool F4, int NB>      // blocks of a CU
 constexpr int kResident = sizeof(T) == 4 && D == 128 ? (NB == 2 ? 2 : 3) : (NB == 1 ? 5 : 4) - (F4 && D == 128);
 template <typename T, int D, bool F4>
-constexpr int kPart = F4 ? 64 : sizeof(T) * D == 128 ? 32 : 16;
+constexpr int kPart = mass_part(F4, F4 ? D / 2 : (int)sizeof(T) * D);
 template <typename T, int D, bool F4, int NB, int S>
 __global__ __launch_bounds__(kThreads, (kResident<T, D, F4, NB>)) void mass_few(PagedView v, MassArgs a,
                                                                           RowList r) {
   constexpr int kTokens = S * kPart<T, D, F4>, kHalves = kPart<T, D, F4> / 16;
+  static_assert(kTokens <= kThreads, "a thread to each token of a tile");
   struct K {
     KRow<T, D, F4> half[kHalves];
   };
@@ -365,7 +365,8 @@ __global__ __launch_bounds__(kThreads, (kResident<T, D, F4, NB>)) void mass_few(
 
 // --------------------------------------------------------------- many rows
 
-constexpr int kTile = 256;         // tokens of a block, 64 to a wave
+constexpr int kTile = kMassTile;   // tokens of a block, 64 to a wave
+static_assert(kTile == kThreads, "a thread to each token of a tile");
 constexpr int kStage = 64;         // rows of a stage
 constexpr int kRing = 3;           // stages in LDS: this one, the next, and one that is loading
 
@@ -761,15 +762,19 @@ int launch_mass_add(const PagedView& v, const MassCall& c, void* stream) {
     return (int)hipGetLastError();
   }
   const size_t lds = (size_t)2 * v.G * c.s.tile * sizeof(float);
+  if (c.s.tile < 1 || lds > 64 * 1024 || c.s.row_blocks < 1 || c.s.row_blocks > 2) return (int)hipErrorInvalidValue;
+  bool made = true;          // a kernel for the division
   const auto by_tile = [&](auto t, auto d, auto f4, auto nb) {
     using T = typename decltype(t)::type;
     constexpr int D = decltype(d)::value, NB = decltype(nb)::value;
     constexpr bool F4 = decltype(f4)::value;
     const unsigned blocks = (unsigned)std::min<int64_t>(c.s.blocks, 256 * kResident<T, D, F4, NB>);
     const auto go = [&](auto kernel) { kernel<<<blocks, kThreads, lds, st>>>(v, a, c.r); };
+    constexpr int kMost = kMassTile / kPart<T, D, F4>;
     if (c.s.tile == kPart<T, D, F4>) go(mass_few<T, D, F4, NB, 1>);
     else if (c.s.tile == 4 * kPart<T, D, F4>) go(mass_few<T, D, F4, NB, 4>);
-    else if constexpr (!F4) go(mass_few<T, D, F4, NB, kThreads / kPart<T, D, F4>>);
+    else if (c.s.tile == kMassTile) go(mass_few<T, D, F4, NB, kMost>);
+    else made = false;
   };
   const auto by_rows = [&](auto t, auto d, auto f4) {
     if (c.s.row_blocks == 1) by_tile(t, d, f4, Int<1>{});
@@ -781,7 +786,7 @@ int launch_mass_add(const PagedView& v, const MassCall& c, void* stream) {
     else by_rows(Type<float>{}, d, std::false_type{});
   };
   v.d == 128 ? by_type(Int<128>{}) : by_type(Int<64>{});
-  return (int)hipGetLastError();
+  return made ? (int)hipGetLastError() : (int)hipErrorInvalidValue;
 }
 
 }  // namespace starkv
