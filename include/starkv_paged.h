@@ -55,7 +55,8 @@ extern "C" {
  * the scale is the 2^e for which a is in (3.5, 7] * 2^e (b clamped to [2, 252]), and
  * an element becomes the nearest of the above times 2^e, ties to the even code,
  * beyond 6 to 6.  A block that holds an infinity or NaN becomes NaN.  Every other
- * block stands for finite bf16 numbers, and the attentions are those over them. */
+ * block stands for finite bf16 numbers, and the attentions are those over them.  In a
+ * pool filled otherwise (bytes 253 and 254) what is 2^128 or more is an infinity. */
 #define STARKV_FP4 4
 
 /* A paged cache.  Token t of the sequence in slot b lies in page

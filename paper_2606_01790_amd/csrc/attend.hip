@@ -158,9 +158,9 @@ __device__ inline void zero_not_finite(R& r) {
 // conversion, two at a time, as the fragments are made, and all else is the
 // same.  K's products may take the elements of a row in any order that Q's take
 // too: lane quad holds the D/4 neighbouring ones that it reads at once, which are
-// of one scale.  A step is a quarter of bf16's bytes for more instructions (219 of
-// vectors and 95 scalar ones for 32 tokens), so its rows are asked for while the
-// step before is worked on.  (Made into bf16 only where they are used, which leaves
+// of one scale.  A step is a quarter of bf16's bytes for more instructions (174 of
+// vectors and 107 scalar ones beside 16 products for 32 tokens), so its rows are asked
+// for while the step before is worked on.  (Made into bf16 only where they are used, which leaves
 // registers for a third block on a CU, they took 95 us of 32 sequences and 129 of 28
 // layers, where this takes 93 and 127.)
 // kOnePage: pages of 32 tokens or more, so that a step lies in one.
@@ -294,6 +294,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
     frag kf[2][NF];
     vrow vv[8][VR::kLoads];
     if constexpr (F4) {
+      // (the empty asm: now, or the words are copied out of the way of the next loads, to be
+      // made into numbers behind them; one token over 13,711 in 28 layers 43 us and not 40)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const float ks = __uint_as_float((uint32_t)ahead.ks[h] << 23);
@@ -303,6 +305,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
           typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
           kf[h][f] = __builtin_bit_cast(frag, u32x4{from_fp4<0>(w, ks), from_fp4<1>(w, ks),
                                                     from_fp4<2>(w, ks), from_fp4<3>(w, ks)});
+          asm volatile("" : "+v"(kf[h][f]));
         }
         // the byte of the lane's columns among each row's scales, turned to where a
         // float's exponent lies; the conversion looks at nothing else of it
@@ -319,6 +322,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
             vv[4 * h + j][0][2] = from_fp4<2>(w, vs);
             vv[4 * h + j][0][3] = from_fp4<3>(w, vs);
           }
+          asm volatile("" : "+v"(vv[4 * h + j][0]));
         }
       }
       page0 = next0;
@@ -425,11 +429,16 @@ __global__ __launch_bounds__(kThreads, 2) void attend_few(PagedView v, AttendArg
               const int col = 16 * VR::kCols * (e / VR::kCols) + VR::kCols * (4 * quad + i) +
                               e % VR::kCols;
               float val;
-              if constexpr (F4)      // a block of 4 bits is NaN or finite as a whole
-                val = (uint8_t)block[v.P * (D / 2) + (t & (v.P - 1)) * (D / 32) + col / 32] == 255
-                          ? __builtin_nanf("") : 0.f;
-              else
+              if constexpr (F4) {    // (scale bytes 253 and 254: some elements of a block are infinite)
+                const uint8_t s = block[v.P * (D / 2) + (t & (v.P - 1)) * (D / 32) + col / 32];
+                val = 0.f;
+                if (s >= 253) {
+                  const uint32_t pair = from_fp4<0>((uint8_t)vr[col / 2], __uint_as_float((uint32_t)s << 23));
+                  val = __uint_as_float(col & 1 ? pair & 0xFFFF0000u : pair << 16);
+                }
+              } else {
                 val = (float)reinterpret_cast<const T*>(vr)[col];
+              }
               if (!(fabsf(val) < INFINITY)) o[nb][e][i] = fmaf(pk, val, o[nb][e][i]);
             }
         }
