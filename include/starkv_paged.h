@@ -332,6 +332,12 @@ starkv_status starkv_mass_fork(const starkv_paged* cache, const int32_t* src, co
  * for, the sequence ends up shorter.  Rows move as with starkv_pages_compact and
  * tail = recent, and the masses with them.  Other sequences stay as they are,
  * STARKV_SEQ_SHORT.
+ * The rows move to pages that were free when the call began, and their own are let
+ * go afterwards: a call takes ceil((sinks + keep + recent) / page_tokens) free pages for
+ * each long sequence (fewer where dropped tokens leave fewer to keep), in order while
+ * they last, and the others get STARKV_SEQ_NO_PAGES.  A full pool evicts nothing, so keep
+ * the pages of one sequence aside: with these, calls of one sequence each can evict all,
+ * as each lets go of no fewer than it took (unless forks share them).
  * slots: no slot twice (E_PARAM).   mass: device, in and out.
  * idx:    device out, int32 [n_layers][n][sinks + keep]: the kept tokens but for
  *         the recent ones, ascending; -1 behind the last, and for short sequences.
