@@ -279,9 +279,10 @@ starkv_status starkv_attend_window(const starkv_paged* cache, const int32_t* slo
  * each attention, starkv_mass_fork each fork, and starkv_pages_evict takes the
  * lightest tokens away, their masses with them.  A token has a mass from the call
  * on whose rows it is one of: it needs no start, and what lies behind a sequence
- * or in a slot in no use is not looked at.  starkv_pages_compact moves no masses;
- * after the compaction of a drafted tree's path, weigh the accepted tokens as rows of
- * a starkv_attend_window call over them. */
+ * or in a slot in no use is not looked at.  starkv_pages_compact moves no masses.
+ * After the compaction of a drafted tree's path, weigh the accepted tokens with their
+ * rows of q and lse of the starkv_attend_tree call, gathered, and no window: where
+ * an accepted row saw its ancestors, they and the prefix are what is before it now. */
 
 /* Add the weights of the last rows[b] >= 0 tokens (host) of each sequence: with
  * x, window, sinks and the tokens V(i) that query token i sees as for
@@ -307,7 +308,8 @@ starkv_status starkv_mass_add(const starkv_paged* cache, const int32_t* slots, i
 
 /* The same behind the grow that made the rows: where grown[b] is not
  * STARKV_SEQ_OK nothing is added and no token is the rows' own, out[t] = mass[t] for
- * all tokens of the sequence.  grown: as for starkv_pages_write_grown.  Errors: as above. */
+ * all tokens of the sequence.  grown: as for starkv_pages_write_grown, or the status of
+ * the compaction behind that grow.  Errors: as above. */
 starkv_status starkv_mass_add_grown(const starkv_paged* cache, const int32_t* slots, int32_t n,
                                     const int32_t* rows, const void* q, const float* lse,
                                     int32_t window, int32_t sinks, int32_t max_len,
