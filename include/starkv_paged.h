@@ -233,7 +233,9 @@ starkv_status starkv_pages_compact_grown(const starkv_paged* cache, const int32_
  * whose logits are all -infinity (from K or q themselves).  Tokens outside
  * V(i), and dropped ones, do not touch row i, whatever their K and V hold
  * (infinities and NaN included).  Softmax, sums and lse are float32 (bf16 and
- * 4-bit caches: the weights are rounded to bf16 for the product with V).
+ * 4-bit caches: the weights are rounded to bf16 for the product with V).  The sums are
+ * of weights relative to the largest so far, 2^8 at most: where 2^8 sum_t |v_t| is 2^128
+ * or more, an output that is finite may overflow on the way.
  * q:   device, the cache's dtype (STARKV_FP4: bf16), [n_layers][sum rows][H][d] contiguous, rows
  *      of the call's sequences in order; 16-byte aligned.
  * out: device out, as q.   lse: device out, float32 [n_layers][sum rows][H],

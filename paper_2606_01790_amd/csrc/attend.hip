@@ -30,8 +30,8 @@
 // 28 layers 271 us (5.8 TB/s), one of each of 16 sequences of 3,000 to 12,000 116
 // (4.2); 4 trees of up to 13 tokens in 4 layers 35, 8 trees of up to 48 over
 // 1,664 to 39,197 tokens 347 (57 TFLOP/s of 154); a chunk of 1,000 tokens behind
-// 12,711 2,502 (76).  4 bits: one token over 40,941 in 28 layers 120 us (624 MB, 5.2
-// TB/s), over 13,711 43, where bf16 takes 143; one of each of 32 sequences of 37 to
+// 12,711 2,502 (76).  4 bits: one token over 40,941 in 28 layers 118 us (624 MB, 5.3
+// TB/s), over 13,711 40, where bf16 takes 143; one of each of 32 sequences of 37 to
 // 40,941 tokens 89 (357 MB, 4.0); over 600 in one layer 11; trees of seven (28 rows
 // of 64 elements) of 16 sequences of 500 to 13,711 tokens 24.
 #include <algorithm>
@@ -158,8 +158,8 @@ __device__ inline void zero_not_finite(R& r) {
 // conversion, two at a time, as the fragments are made, and all else is the
 // same.  K's products may take the elements of a row in any order that Q's take
 // too: lane quad holds the D/4 neighbouring ones that it reads at once, which are
-// of one scale.  A step is a quarter of bf16's bytes for more instructions (174 of
-// vectors and 107 scalar ones beside 16 products for 32 tokens), so its rows are asked
+// of one scale.  A step is a quarter of bf16's bytes for more instructions (201 of
+// vectors, 16 products among them, and 97 scalar ones for 32 tokens), so its rows are asked
 // for while the step before is worked on.  (Made into bf16 only where they are used, which leaves
 // registers for a third block on a CU, they took 95 us of 32 sequences and 129 of 28
 // layers, where this takes 93 and 127.)

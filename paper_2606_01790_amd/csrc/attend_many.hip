@@ -29,8 +29,9 @@
 // instructions to each against one.  LDS has no bank conflicts.  Short calls are
 // bound by their chain of loads (eight tokens over 600: 9 us, and 3 to join).
 // 4 bits, which pass through registers on their way to LDS: 2,755 tokens appended to
-// 10,956 418 us (800 TFLOP/s); trees of 24 tokens over 13,711 in 28 layers 238 (555;
-// 168 rows in the place of 256, as in bf16, which takes 236); of 64 over 40,941 1,213.
+// 10,956 408 to 418 us (800 to 820 TFLOP/s; matrix units and vector work 35 and 38% of the
+// cycles, and a quarter neither); trees of 24 tokens over 13,711 in 28 layers 235 to 238
+// (560; 168 rows in the place of 256, as in bf16, which takes 236); of 64 over 40,941 1,213.
 #include <algorithm>
 
 #include "attend.h"
@@ -97,7 +98,8 @@ __device__ inline void stage(const char* from, int64_t ts, uint32_t row, uint32_
 // The same of a 4-bit cache, whose elements become bf16 on their way: a lane
 // takes the four bytes of a piece, and the byte of its scale, into registers a
 // step before they go to LDS.  One conversion of a number for all rows of a block:
-// 7.7 vector instructions to each product where bf16 has 6.6, and LDS written by them.
+// 7.7 vector instructions to each product, itself among them, where bf16 has 6.6, and LDS
+// written by them.
 template <int D>
 struct Fp4Group {
   static constexpr int kLoads = 16 * D * 2 / 1024, kRows = 16 / kLoads, NP = D / 8;

@@ -217,10 +217,10 @@ __device__ __forceinline__ void select(const PagedView& v, const EvictArgs& a, i
     f.T = 1;
   } else {
     while (!f.done() && f.met - f.over > kCands) {
-      if (N > 0 || f.bit == 0) {
+      if constexpr (N > 0) {
         f.settle(block_totals(sh[turn++ & 1], keys.at_least(f.next())).a);
       } else {
-        // two bits of a pass over keys that are read again
+        // two bits of a pass over keys that are read again (31 and 30, 29 and 28, ..)
         const uint32_t half = 1u << (f.bit - 1);
         int c[3];
         keys.at_least({f.T | half, f.T | 2 * half, f.T | 3 * half}, c);

@@ -19,11 +19,11 @@
 // layers 137 us (754 MB, 5.5 TB/s; a copy makes 4.9), of 32 sequences of 37 to 40,941
 // in one layer 125 in bf16 (5.5), 43 in 4 bits, 242 in float32; one over 13,711 in 28
 // layers 74, 26 and 143, four 85, 40 and 201.  4 bits are bound by what the waves issue.
-// Many rows, with the join (5 us): 2,755 over 13,711 tokens 276 us (244 GFLOP, 880
-// TFLOP/s), in 4 bits 260, in float32 2,330 (104; a library product makes 154); all of
-// 8,192 335 (720); 16 rows over 13,711 in 28 layers 125, 93 and 490.  The matrix units
-// are busy in 40% of the SIMDs' cycles, as in the attention of many rows, and for the
-// same reason: 8.7 vector instructions to a product.
+// Many rows, with the join (5 us): 2,755 over 13,711 tokens 264 to 276 us (244 GFLOP, 880 to
+// 920 TFLOP/s), in 4 bits 260, in float32 2,284 (107; a library product makes 154); all of
+// 8,192 335 (720); 16 tokens' rows over 13,711 in 28 layers 125, 93 and 498.  The matrix units
+// are busy in 41% of the SIMDs' cycles, as in the attention of many rows, and for the
+// same reason: 8.9 vector instructions to a product, itself among them, which fill the rest.
 #include <algorithm>
 #include <type_traits>
 

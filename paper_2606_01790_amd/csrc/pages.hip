@@ -217,7 +217,7 @@ constexpr bool kScaled = VPR <= 4;
 
 // Rows [0, part) of a replaced page, one (sequence, group, layer) per block (16
 // forks with 28 or 35 rows in 28 layers: 10.4 us, 5.6 TB/s read and written;
-// with nothing to copy 2).
+// with nothing to copy 2; with 35 rows 10 in bf16, 17 in float32, 5 in 4 bits).
 template <int VPR>
 __global__ __launch_bounds__(256) void grow_copy(PagedView v, const i32x4* info) {
   const i32x4 c = info[blockIdx.x];
@@ -346,8 +346,8 @@ __global__ __launch_bounds__(256) void write_fp4(PagedView v, Rows<N> r, WriteAr
 
 // The rows of tokens out of their pages, 16 bytes of K and of V per thread; of a
 // 4-bit cache the bf16 numbers that four bytes stand for.  What has no page gives
-// zeros.  Bound by HBM: 13,711 tokens in 28 layers out of 4 bits 150 us (995 MB, 6.6
-// TB/s), 237 with the rows written through the caches, where they took the place of the
+// zeros.  Bound by HBM: 13,711 tokens in 28 layers of bf16 254 us (1,572 MB, 6.2 TB/s), of
+// float32 512 (6.1), out of 4 bits 150 (995 MB, 6.6), 237 with the rows written through the caches, where they took the place of the
 // pages.
 struct ReadArgs {
   char* k;
@@ -542,7 +542,8 @@ struct MoveArgs {
 
 // The kept rows into the fresh pages, one vector of K and of V per thread
 // (28 layers, 2,723 rows kept of 13,711: 49 us, 6.5 TB/s read and written; four
-// vectors per thread with ordinary stores 61, against 52 on that card).  The rows
+// vectors per thread with ordinary stores 61, against 52 on that card; of 128 elements
+// in float32 101, in 4 bits 22, and of 64 in 4 bits 17, with their scales).  The rows
 // are not read again here, so the stores bypass the caches.
 template <int VPR, int N>
 __global__ __launch_bounds__(256) void compact_move(PagedView v, Seqs<N> s, MoveArgs m) {
